@@ -214,6 +214,124 @@ int fa_bwd_gqa(const void* q, const void* k, const void* v, const void* o, const
                int B, int H, int H_kv, int N, int d, float scale, int causal, int dtype, void* stream);
 
 /*
+ * Rotary positions.  The first rot_dim elements of a row are turned in pairs by an angle that grows with the token's position,
+ * the others are passed on as they are:
+ *     phi_i = position * inv_freq[i],   y_a = A (x_a cos phi_i - x_b sin phi_i),   y_b = A (x_a sin phi_i + x_b cos phi_i)
+ * where pair i < rot_dim / 2 is (a, b) = (2i, 2i + 1) with interleaved = 1 and (i, i + rot_dim / 2) with interleaved = 0.
+ * fa_rope_bwd turns gradients: the transpose, which is the same with the sign of every angle changed.
+ *   q, k     : [B,H,N,d] and [B,H_kv,N,d] of dtype FA_F32, FA_BF16 or FA_F16 (device, read); k NULL: q alone (k_out, its
+ *              strides and H_kv are ignored)
+ *   q_out, k_out : the same shapes and dtype (device, written); q_out may be q and k_out may be k, with the same strides.  Any
+ *              other overlap gives undefined results.
+ *   *_strides: three numbers on the HOST, in elements, of a tensor's batch, head and token dimension (its d elements are
+ *              contiguous), or NULL for a contiguous tensor.  At least 0 (of an output: d) and multiples of 16 bytes, else
+ *              FA_ERR_SHAPE and FA_ERR_ALIGN; of a dimension of size 1 anything.  (So a projection's [B,N,H,d] is rotated
+ *              without a transposed copy of it.)
+ *   inv_freq : fp64 [rot_dim / 2], radians per token (device, read); fa_rope_frequencies computes the usual ones.  Angles
+ *              are computed and reduced in 64 bits, so far positions are as exact as near ones.
+ *   positions: int32 [B,N], any value (device, read), or NULL: token n of every sequence stands at n
+ *   rot_dim  : a positive multiple of 16, at most d (else FA_ERR_UNSUPPORTED; not positive or above d: FA_ERR_SHAPE)
+ *   amplitude: A, finite and > 0 (1 without one)
+ * Products and sums are fp32, rounded once.  Of the arrays of this call and those below, fp64, fp32 and int32 ones (inv_freq,
+ * positions, scales, lse, tables, lengths) need the alignment of their type only.
+ */
+int fa_rope(const void* q, const long long* q_strides, const void* k, const long long* k_strides,
+            void* q_out, const long long* q_out_strides, void* k_out, const long long* k_out_strides,
+            const double* inv_freq, const int* positions, int B, int H, int H_kv, int N, int d, int rot_dim,
+            float amplitude, int interleaved, int dtype, void* stream);
+
+int fa_rope_bwd(const void* dq, const long long* dq_strides, const void* dk, const long long* dk_strides,
+                void* dq_out, const long long* dq_out_strides, void* dk_out, const long long* dk_out_strides,
+                const double* inv_freq, const int* positions, int B, int H, int H_kv, int N, int d, int rot_dim,
+                float amplitude, int interleaved, int dtype, void* stream);
+
+/*
+ * Frequencies of rotary positions, and their scaling for contexts longer than the trained one.  Host only.  With
+ * f_i = base^(-2i / rot_dim), s = factor and n_i = trained_len f_i / (2 pi), how often pair i turns over the trained length:
+ *     FA_ROPE_PLAIN     f_i                                         (factor and trained_len are ignored)
+ *     FA_ROPE_LINEAR    f_i / s                                     (positions interpolated)
+ *     FA_ROPE_NTK       (base s^(rot_dim / (rot_dim - 2)))^(-2i / rot_dim)  (a larger base)
+ *     FA_ROPE_BY_PARTS  f_i (g + (1 - g) / s), g = clamp((n_i - 1) / 31, 0, 1)  (arXiv 2309.00071, alpha 1 and beta 32: what
+ *                       turns often is kept, what is slow is interpolated)
+ *   inv_freq  : rot_dim / 2 doubles on the HOST (written)
+ *   amplitude : one float on the HOST (written), or NULL: the factor A that goes with it, 0.1 ln s + 1 by parts, 1 otherwise
+ * rot_dim even and > 0 (NTK: > 2), base > 1, factor >= 1 and trained_len > 0, all finite; else FA_ERR_SHAPE.
+ */
+typedef enum { FA_ROPE_PLAIN = 0, FA_ROPE_LINEAR = 1, FA_ROPE_NTK = 2, FA_ROPE_BY_PARTS = 3 } fa_rope_scaling;
+
+int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double base, int scaling, double factor,
+                        double trained_len);
+
+/*
+ * A paged cache of keys and values.
+ *   k_pages, v_pages : [n_pages, H_kv, page_size, d] of cache_dtype FA_BF16, FA_F16 or FA_FP8_E4M3, contiguous
+ *   k_scales, v_scales : fp32 [n_pages, H_kv, page_size] with FA_FP8_E4M3, where the cached value is code * scale of its
+ *                 token and head; NULL otherwise (given with a 16-bit cache: FA_ERR_DTYPE)
+ *   block_table : int32 [B, max_pages]; token p of sequence b is in slot p % page_size of page block_table[b][p / page_size]
+ *   lens        : int32 [B], how many tokens of a sequence the cache holds (less than 0: none)
+ * all on the device.  page_size: a multiple of 16 (else FA_ERR_UNSUPPORTED) with 4 page_size d <= 0x7ff00000; a cache that is
+ * one contiguous [B, H_kv, max_tokens, d] is one of B pages.  A sequence has max_pages * page_size places (< 2^31).  A page
+ * may stand in several sequences' rows of the table.
+ * A table entry outside 0 .. n_pages - 1 is no page: nothing is written to it, and its tokens are neither read back nor seen.
+ * The same goes for tokens at or past max_pages * page_size.
+ *
+ * fa_cache_write: token t < counts[b] of k and v goes to place lens[b] + t of sequence b (lens is not changed).  No two tokens
+ * of a call may go to the same slot of the same page, or that slot's contents are undefined.
+ *   k, v    : [B,H_kv,T,d] of in_dtype FA_F32, FA_BF16 or FA_F16 (device, read); strides as in fa_rope
+ *   counts  : int32 [B] (device), or NULL: T of every sequence.  (Above T counts as T.)
+ * A 16-bit cache takes its own type, or fp32, which is rounded to nearest even (another 16-bit type: FA_ERR_UNSUPPORTED).
+ * In an e4m3 cache a token of one head gets
+ *     scale = a / 448,   code = round-to-nearest-even e4m3 of clamp(x * (448 / a), +-448),   a = max |x| over its finite elements
+ * (a = 0: scale 1; 0 < a < 2^-100: a = 2^-100).  So an infinity becomes the largest value of the token, and a NaN stays one.
+ */
+int fa_cache_write(const void* k, const long long* k_strides, const void* v, const long long* v_strides,
+                   void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                   const int* block_table, const int* lens, const int* counts, int B, int H_kv, int T, int d,
+                   int page_size, int n_pages, int max_pages, int in_dtype, int cache_dtype, void* stream);
+
+/*
+ * The cache back as dense tensors: the first min(lens[b], N) tokens of every sequence, code * scale rounded once.
+ *   k, v    : [B,H_kv,N,d] of out_dtype, contiguous (device, written); rows from lens[b] on and rows of what is no page stay
+ *             as they are
+ * out_dtype: FA_F32, FA_BF16 or FA_F16; a 16-bit cache is read as its own type or FA_F32 (else FA_ERR_UNSUPPORTED).
+ */
+int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                  const int* block_table, const int* lens, void* k, void* v, int B, int H_kv, int N, int d,
+                  int page_size, int n_pages, int max_pages, int cache_dtype, int out_dtype, void* stream);
+
+/*
+ * Attention of T new tokens of every sequence over the cache, which already holds their keys and values too (fa_cache_write
+ * with the same lens and counts): one token for ordinary decoding, several for a chunk of a prompt or a tree of drafted tokens.
+ * New token t sees the places 0 .. lens[b] - 1, and place lens[b] + u of new token u < counts[b] where
+ *     tree == NULL: u <= t;   otherwise: bit u % 32 of word u / 32 of its row of `tree` is set.
+ *   q       : [B,H,T,d] of dtype FA_BF16 or FA_F16 (device, read); strides as in fa_rope.  Query head h reads key/value head
+ *             h / (H / H_kv).
+ *   tree    : int32 [tree_batches, T, ceil(T / 32)] (device, read), tree_batches = B, or 1 where all sequences share one
+ *   o       : the shape and dtype of q (device, written), strides as in fa_rope; lse : fp32 [B,H,T], contiguous (device, written)
+ *             A row that sees nothing gets O = 0 and L = -infinity.  Rows of tokens from counts[b] on stay as they are.
+ *   cache_dtype : dtype, or FA_FP8_E4M3 (another: FA_ERR_UNSUPPORTED)
+ *   max_len : what lens[b] + T is expected to reach at most, or 0: max_pages * page_size.  It decides how the keys are
+ *             divided over the chip and with that the time, not which of them are seen.  fa_fwd_cache_workspace_bytes takes
+ *             the same number, and max_pages * page_size in place of 0.
+ *   workspace : device scratch of at least fa_fwd_cache_workspace_bytes(...) bytes (which can be 0: then it may be NULL), 16-byte
+ *             aligned, owned by the caller; calls that may run at the same time need one each.
+ * T <= FA_CACHE_MAX_TOKENS (else FA_ERR_TOO_LARGE).  A value or scale in a place that a row does not see, whatever it is,
+ * has no influence on the row.  Scores, softmax and the sums are fp32; the probabilities are rounded to the cache's 16-bit
+ * type (fp16 with FA_FP8_E4M3) for their product with V.  Nothing is accumulated with atomics: results are bit-for-bit
+ * repeatable.
+ */
+#define FA_CACHE_MAX_TOKENS 256
+
+size_t fa_fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype);
+
+int fa_fwd_cache(const void* q, const long long* q_strides, const void* k_pages, const void* v_pages,
+                 const float* k_scales, const float* v_scales, const int* block_table, const int* lens, const int* counts,
+                 const int* tree, int tree_batches, void* o, const long long* o_strides, float* lse,
+                 void* workspace, size_t workspace_bytes, int B, int H, int H_kv, int T, int d,
+                 int page_size, int n_pages, int max_pages, int max_len, float scale, int dtype, int cache_dtype,
+                 void* stream);
+
+/*
  * Measurement aid, not part of the attention path: the rate of the matrix pipes alone.  The
  * roofline fractions of the kernels above are quoted against the published MFMA peak; this
  * call measures what the chip sustains when every wave issues only independent MFMAs

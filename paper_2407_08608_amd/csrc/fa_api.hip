@@ -5,6 +5,7 @@
 
 #include <atomic>
 
+#include "fa_check.h"
 #include "fa_launch.h"
 
 // Scratch of fa_bwd_noalloc: the backward's D = rowsum(dO o O) vector.  A file-scope device array, so
@@ -31,13 +32,6 @@ void* noalloc_scratch_on_current_device() {
     g_scratch_ptr[dev].store(p, std::memory_order_release);
     return p;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
-
-// A sticky error left on this thread by earlier, unrelated HIP work would otherwise be reported by the
-// first hipGetLastError() after our own launch and be mistaken for ours.
-void forget_stale_hip_error() { (void)hipGetLastError(); }
 
 int check_common(int B, int H, int N, int d, float scale, int causal) {
     if (B <= 0 || H <= 0 || N <= 0 || d <= 0) return FA_ERR_SHAPE;

@@ -342,6 +342,33 @@ size_t bwd_workspace_bytes(int B, int H, int N, int d);
 int launch_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout,
                void* dq, void* dk, void* dv, void* workspace, int B, int H, int H_kv, int N, int d, float scale,
                int causal, int dtype, hipStream_t stream);
+
+// Rows of d contiguous elements in a tensor with batch, head and token dimensions; strides in elements
+struct Rows {
+    const void* p;
+    long batch, head, token;
+};
+
+int launch_rope(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
+                int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved, bool transposed, int dtype,
+                hipStream_t stream);
+
+// A paged cache (include/fa_mi355.h): pages [n_pages][H_kv][page_size][d], scales without the last dimension, NULL for 16 bits
+struct Cache {
+    void *k, *v;
+    float *k_scales, *v_scales;
+    const int *block_table, *lens;
+    int H_kv, page_size, n_pages, max_pages, dtype;
+};
+
+int launch_cache_write(const Rows& k, const Rows& v, const Cache& cache, const int* counts, int B, int T, int d, int in_dtype,
+                       hipStream_t stream);
+int launch_cache_read(const Cache& cache, void* k, void* v, int B, int N, int d, int out_dtype, hipStream_t stream);
+
+size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype);
+int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
+                     void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream);
+
 int launch_probe_mfma(const void* operands, size_t operand_bytes, float* sink, int iters, bool fp8, hipStream_t stream);
 double probe_mfma_flops(int iters, bool fp8);
 
