@@ -31,7 +31,7 @@ def _compile(src):
 
 # Sources with MFMAs or loads written as inline assembly: their device assembly is generated once more as text and checked
 # for instructions that touch an MFMA result, or write what such an instruction reads, too close to it (mfma_hazard_check.py).
-HAZARD_CHECKED = ["fa_bwd.hip", "fa_fwd.hip", "fa_fwd_fp8.hip"]
+HAZARD_CHECKED = ["fa_bwd.hip", "fa_fwd.hip", "fa_fwd_cache.hip", "fa_fwd_fp8.hip"]
 
 
 def _check_hazards(name):
