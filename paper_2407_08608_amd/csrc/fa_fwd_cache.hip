@@ -1,23 +1,27 @@
 // Attention of the new tokens of every sequence over a paged cache (include/fa_mi355.h: fa_fwd_cache).
 //
-// The rows that read one key/value head, (query head of the group) x (new token), are queries of one dense problem: 32 of them
-// make a tile (lane column = row), RT tiles a workgroup.  The keys of a sequence are divided into chunks, a workgroup each; the
-// NW waves of a workgroup take the chunk's 32-key tiles in turn, each with a softmax state and an output accumulator of its
-// own, and meet in the LDS at the end, in a fixed order.  Where a sequence has several chunks the workgroup leaves (sum p v,
-// reference, sum p) in the workspace and a second launch joins them, in a fixed order too.
+// The rows that read one key/value head, (query head of the group) x (new token), are queries of one dense problem: COLS of them
+// (16, or 32) make a tile, one to a lane column, RT tiles a workgroup.  The keys go to workgroups in steps of NW tiles of 32 keys,
+// a tile for each wave, which has a softmax state and an output accumulator of its own; they meet in the LDS at the end, in a
+// fixed order.
 //
 // Bound by HBM up to about 300 rows to a key/value head (4 rows d flops for 4 d bytes of a key): the cache is read once per
-// row group, straight into the LDS, and as much of it as the LDS holds is on its way at any time.  A wave stages its own tiles
-// (no barrier in the loop): a slot for K and one for V, STG deep, refilled as soon as the wave has read them, so requests go
-// on while scores, softmax and products are computed.
+// row group, straight into the LDS.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
+//   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
+//     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
+//     has of such a one, (sum p v, reference, sum p), goes to the workspace, and a second launch joins it with what the teams
+//     before and after have, in that order.  Where there is nothing to even out a workgroup has a whole sequence and head.
 //   - Pages: 16 consecutive places lie in one page (page_size is a multiple of 16), so a tile has two resources.  Lane i of a
 //     wave looks up the two rows of the wave's i-th tile, 64 tiles at a time; what is no page, or past the last key, gets a
 //     resource of length 0 and arrives as zeros.
 //   - Masks: only tiles that reach the new tokens (or hold a bad page) look at one.  What a lane's row sees of a tile is a 32-bit
 //     word: places before the new tokens, the row's window of the tree, the tokens that are there.
 //   - e4m3: codes become 16-bit operands in registers (exact): K in the type of Q, with the key's scale on the score; V in
-//     fp16, with P~ = p (v scale / F), F a power of two not below the scales so far.  So P~ is at most 2^kLazyLog2 in fp16 whatever
+//     fp16, with P~ = p (v scale / F), F a power of two not below the scales so far.  So P~ is at most 2^kLazy in fp16 whatever
 //     the scales are, and eleven bits of each weight reach the product.
+//   - 16 columns where a group has no more rows (v_mfma_16x16x32 instead of 32x32x16): half the registers, matrix and vector
+//     instructions for a tile.
 #include "fa_device.h"
 #include "fa_launch.h"
 
@@ -27,8 +31,11 @@ struct CachedArgs {
     Rows q, o;
     Cache c;
     const int *counts, *tree;
-    float *lse, *part, *state;  // part, state: the workspace, [split][B H T][D] and [split][B H T][2]
-    int B, H, T, tree_batches, row_groups, splits, chunk;  // chunk: keys, a multiple of 32
+    float* lse;
+    // the workspace: first steps of the sequences [B + 1], then for each workgroup two segments [rows][D] and [rows][2]
+    long* first_step;
+    float *part, *state;
+    int B, H, T, tree_batches, row_groups, teams;  // teams 0: a workgroup to a sequence, head and row group
     float scale;
 };
 
@@ -51,70 +58,169 @@ struct Extent {
         count = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
         keys = len + min(count, places - len);
     }
-    __device__ __forceinline__ int splits(const CachedArgs& a) const {  // the last chunk takes what is left
-        const int n = (keys + a.chunk - 1) / a.chunk;
-        return min(max(n, 1), a.splits);
+    template <int STEP>
+    __device__ __forceinline__ int steps() const {  // at least one: rows that see nothing are written too
+        return keys <= STEP ? 1 : (int)(((unsigned)keys + STEP - 1) / STEP);
     }
 };
 
-// A wave's tiles of 32 keys in the LDS, as they are staged and read: 16-bit elements like WaveTile, or codes.  A tile is
-// unpadded; 16-byte chunk c of row r sits at c ^ swizzle(r), applied through the global address that a lane fetches.
-template <typename Tag, int D, bool CODES>
-struct CacheTile {
-    static constexpr int ROWB = D * (CODES ? 1 : 2), TILE_B = 32 * ROWB, CPR = ROWB / 16, RPI = 1024 / ROWB, NI = 32 / RPI;
-    static constexpr int KR = CODES ? D / 32 : D / 16, DT = D / 32, TR = CODES ? 1 : 2;
-    uint32_t base;
-    int src[NI / 2];           // byte offset within 16 rows for a staging instruction
-    uint32_t row_at[KR];       // row operands: lane (col, half), chunk 2 k + half of row col
-    uint32_t tr_at[DT][TR];    // transposed operands of rows 0..15
+static __device__ __forceinline__ long readlane64(long v, int lane) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return (long)((uint64_t)lo | (uint64_t)hi << 32);
+}
 
-    // Codes: row reads take one chunk of 16 rows, transposing reads two neighbouring chunks of rows 4 h .. 4 h + 3 and 8 more; both
-    // hit every bank once if bits 0, 1 and 3 of the row, where they do not choose the bank already, move chunk pairs.
-    static __device__ __forceinline__ int swizzle(int r) {
-        if constexpr (!CODES) return WaveTile<D>::swizzle(r);
-        else if constexpr (D == 64) return (r >> 2) & 3;
-        else if constexpr (D == 128) return ((r >> 1) & 1) << 1 | ((r >> 3) & 1) << 2 | ((r >> 2) & 1);
-        else return (r & 1) << 1 | ((r >> 1) & 1) << 2 | ((r >> 3) & 1) << 3 | ((r >> 2) & 1);
+// Calls f(b, steps before sequence b, of all heads) by lane over all sequences, 64 at a time, until it returns true; returns the
+// steps of all sequences that were looked at.
+template <int STEP, typename F>
+static __device__ __forceinline__ long scan_steps(const CachedArgs& a, int lane, F&& f) {
+    long before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        long n = 0;
+        if (b < a.B) n = (long)Extent(a, b).steps<STEP>() * a.c.H_kv;
+        long upto = n;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) {
+            const long y = __shfl_up(upto, x);
+            if (lane >= x) upto += y;
+        }
+        const bool done = f(b, before + upto - n, n);
+        before += readlane64(upto, 63);
+        if (done) break;
     }
+    return before;
+}
+
+// x of this lane's row of 16 lanes and of the row next to it (rows 0 and 1, 2 and 3)
+static __device__ __forceinline__ HalfPair both_rows(float x) {
+    uint32_t a = __builtin_bit_cast(uint32_t, x);
+    uint32_t b = a;
+    asm volatile("" : "+v"(b));
+    auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    uint32_t r0 = r[0], r1 = r[1];
+    asm volatile("" : "+v"(r0), "+v"(r1));
+    return {__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)};
+}
+
+// Eight codes as eight 16-bit elements
+template <typename Tag>
+static __device__ __forceinline__ i32x4 from_codes(int lo, int hi) {
+    i32x4 w;
+    if constexpr (std::is_same_v<Tag, bf16_tag>) {
+        w[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+        w[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+        w[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+        w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+    } else {
+        w[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+        w[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+        w[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+        w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    }
+    return w;
+}
+
+// The two shapes of the matrix products, by the columns (queries) of a tile.  Lane (col, part): col = lane % COLS.
+//   scores      NS values of the lane's query: register r belongs to key (part << SHIFT) + bit(r) of the tile's 32
+//   products    NT accumulators; register r of accumulator dt is output column dt WIDTH + column(r, part)
+template <typename Tag, int D, int COLS> struct Matrix;
+template <typename Tag, int D> struct Matrix<Tag, D, 32> {
+    static constexpr int PARTS = 2, NS = 16, SHIFT = 2, NT = D / 32, WIDTH = 32, SLABS = 2, TILES = 1;
+    typedef f32x16 Acc;
+    static constexpr __device__ int bit(int r) { return 8 * (r >> 2) + (r & 3); }
+    static __device__ __forceinline__ Acc mma(i32x4 a, i32x4 b, Acc c) { return Elem<Tag>::mma(a, b, c); }
+    static __device__ __forceinline__ float max_parts(float x) { return max_both_halves(x); }
+    static __device__ __forceinline__ float sum_parts(float x) { return sum_both_halves(x); }
+};
+template <typename Tag, int D> struct Matrix<Tag, D, 16> {
+    // rows of the two score tiles are dealt so that a part's keys are eight consecutive ones: row i of tile kt is key
+    // 8 (i / 4) + 4 kt + i % 4
+    static constexpr int PARTS = 4, NS = 8, SHIFT = 3, NT = D / 16, WIDTH = 16, SLABS = 1, TILES = 2;
+    typedef f32x4 Acc;
+    static constexpr __device__ int bit(int r) { return r; }
+    static __device__ __forceinline__ Acc mma(i32x4 a, i32x4 b, Acc c) {
+        if constexpr (std::is_same_v<Tag, bf16_tag>)
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float max_parts(float x) {
+        const HalfPair p = both_rows(x);
+        return max_both_halves(fmaxf(p.lo, p.hi));
+    }
+    static __device__ __forceinline__ float sum_parts(float x) {
+        const HalfPair p = both_rows(x);
+        return sum_both_halves(p.lo + p.hi);
+    }
+};
+
+// A wave's tiles of 32 keys in the LDS, as they are staged and read.  A tile is unpadded; 16-byte chunk c of row r sits at
+// c ^ swizzle(r), applied through the global address that a lane fetches, so that each 16 lanes of a row read (16 rows, one
+// chunk) and each 32 of a transposing read (8 rows, two chunks, or 4 and 4, or 16 and 1) hit every bank once, with rows of 64 to
+// 512 bytes.  Everything but the row is a constant that an exclusive or brings in: one address register for each kind of read.
+template <typename Tag, int D, bool CODES, int COLS>
+struct CacheTile {
+    using M = Matrix<Tag, D, COLS>;
+    using PE = std::conditional_t<CODES, f16_tag, Tag>;  // of the product with V
+    using PM = Matrix<PE, D, COLS>;
+    static constexpr int ROWB = D * (CODES ? 1 : 2), TILE_B = 32 * ROWB, CPR = ROWB / 16, RPI = 1024 / ROWB, NI = 32 / RPI;
+    static constexpr int MASK = CPR < 16 ? CPR - 1 : 15;
+    static constexpr int KR = CPR / M::PARTS;  // row reads of a lane and score tile
+    uint32_t base, src0, row0, tr0;
+
+    static constexpr __device__ __host__ int swizzle(int r) {
+        return ((r & 1) << 3 | (r >> 1 & 1) << 2 | (r >> 3 & 1) << 1 | ((r >> 2 ^ r >> 4) & 1)) & MASK;
+    }
+    // what bringing chunk c into an address of row r, or adding row bits that r has not, does to it
+    static constexpr __device__ uint32_t flip(int chunk, int more_rows) { return (uint32_t)((chunk & MASK) ^ swizzle(more_rows)) << 4; }
+    static constexpr __device__ uint32_t plus(int chunk, int more_rows) { return (uint32_t)(more_rows * ROWB + (chunk & ~MASK) * 16); }
+
     __device__ __forceinline__ CacheTile(uint32_t at, int lane) : base(at) {
-        const int col = lane & 31, half = lane >> 5, in = lane & 15, blk = (lane >> 4) & 1;
-#pragma unroll
-        for (int i = 0; i < NI / 2; ++i) {
-            const int r = i * RPI + lane / CPR;
-            src[i] = r * ROWB + ((lane % CPR) ^ swizzle(r)) * 16;
-            asm volatile("" : "+v"(src[i]));
+        const int col = lane % COLS, part = lane / COLS, in = lane & 15, blk = (lane >> 4) & 1;
+        const int r = lane / CPR;
+        src0 = r * ROWB + (((lane % CPR) ^ swizzle(r)) << 4);
+        const int kr = COLS == 32 ? col : 8 * (col >> 2) + (col & 3);
+        row0 = at + kr * ROWB + ((part ^ swizzle(kr)) << 4);
+        if constexpr (CODES) {  // lanes 2 i, 2 i + 1 of 16 point at row i of the group's eight
+            const int i = in >> 1, tr = COLS == 32 ? 4 * part + (i & 3) + 8 * (i >> 2) : 8 * part + i;
+            tr0 = at + tr * ROWB + (((COLS == 32 ? blk : 0) ^ swizzle(tr)) << 4) + 8 * (in & 1);
+        } else {  // lanes 4 i .. 4 i + 3 of 16 point at row i of the group's four
+            const int quad = in & 3, tr = (COLS == 32 ? 4 : 8) * part + (in >> 2);
+            tr0 = at + tr * ROWB + (((COLS == 32 ? 2 * blk : 0) + (quad >> 1)) ^ swizzle(tr)) * 16 + 8 * (quad & 1);
         }
-#pragma unroll
-        for (int k = 0; k < KR; ++k) {
-            row_at[k] = at + col * ROWB + (((2 * k + half) ^ swizzle(col)) << 4);
-            asm volatile("" : "+v"(row_at[k]));
-        }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int hi = 0; hi < TR; ++hi) {
-                if constexpr (CODES) {  // lanes 2 i, 2 i + 1 of 16 point at row i of the group's eight
-                    const int i = in >> 1, r = 4 * half + (i & 3) + 8 * (i >> 2);
-                    tr_at[dt][hi] = at + r * ROWB + (((2 * dt + blk) ^ swizzle(r)) << 4) + 8 * (in & 1);
-                } else {
-                    const int quad = in & 3, r = 4 * half + (in >> 2) + 8 * hi;
-                    tr_at[dt][hi] = at + r * ROWB + (((4 * dt + 2 * blk + (quad >> 1)) ^ swizzle(r)) << 4) + 8 * (quad & 1);
-                }
-                asm volatile("" : "+v"(tr_at[dt][hi]));
-            }
+        asm volatile("" : "+v"(src0), "+v"(row0), "+v"(tr0));
     }
     // All instructions that bring a tile, 16 rows from each resource
     __device__ __forceinline__ void request(const BufferWords (&rsrc)[2], uint32_t offset) const {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) global_to_lds_16B(rsrc[i / (NI / 2)], base + offset + i * 1024, src[i % (NI / 2)]);
+        static_for<NI>([&](auto n) __attribute__((always_inline)) {
+            constexpr int i = decltype(n)::value, r = i * RPI;
+            global_to_lds_16B(rsrc[i / (NI / 2)], base + offset + i * 1024, (int)((src0 ^ (uint32_t)(swizzle(r) << 4)) + (r % 16) * ROWB));
+        });
+    }
+    // the lane's 16 bytes k of its row in score tile kt
+    template <int K, int KT>
+    __device__ __forceinline__ i32x4 row_read(uint32_t offset) const {
+        return lds_load_16B((row0 ^ flip(M::PARTS * K, 4 * KT)) + (offset + plus(M::PARTS * K, 4 * KT)));
+    }
+    // the A operand of V^T: accumulator dt, keys of slab `slab`; codes: their eight bytes
+    template <int DT, int SLAB>
+    __device__ __forceinline__ i32x4 columns(uint32_t offset) const {
+        if constexpr (CODES) {
+            constexpr int chunk = COLS == 32 ? 2 * DT : DT;
+            const i32x2 c = lds_read_tr8((tr0 ^ flip(chunk, 16 * SLAB)) + (offset + plus(chunk, 16 * SLAB)));
+            return i32x4{c[0], c[1], 0, 0};
+        } else {
+            constexpr int chunk = COLS == 32 ? 4 * DT : 2 * DT, more = 16 * SLAB, upper = more + (COLS == 32 ? 8 : 4);
+            const i32x2 lo = lds_read_tr16((tr0 ^ flip(chunk, more)) + (offset + plus(chunk, more)));
+            const i32x2 hi = lds_read_tr16((tr0 ^ flip(chunk, upper)) + (offset + plus(chunk, upper)));
+            return i32x4{lo[0], lo[1], hi[0], hi[1]};
+        }
     }
 
     // An infinity or a NaN in V of a new token is no business of the rows that do not see it, and a product with P = 0 would
     // make it theirs.  So where a tile has one (not_finite), matrix products of ones count for each row and column what it sees
     // of them (add_not_finite), and it is a zero for the product with P (clear_not_finite).
-    using PE = Elem<std::conditional_t<CODES, f16_tag, Tag>>;
     static constexpr int EXPONENT = CODES ? 0x7F7F7F7F : std::is_same_v<Tag, bf16_tag> ? 0x7F807F80 : 0x7C007C00;
-    static constexpr int ONE = !CODES && std::is_same_v<Tag, bf16_tag> ? 0x3F803F80 : 0x3C003C00;  // two ones
+    static constexpr int ONE = std::is_same_v<PE, bf16_tag> ? 0x3F803F80 : 0x3C003C00;  // two ones
     // the elements of a word that are not finite, all bits of each
     static __device__ __forceinline__ uint32_t odd_ones(uint32_t w) {
         const uint32_t x = (w & EXPONENT) ^ EXPONENT;  // 0 where the exponent (of a code: all but the sign) is full
@@ -131,17 +237,6 @@ struct CacheTile {
         const uint32_t sign = ((w & 0x80008000u) >> 15) * 0xFFFFu;
         const uint32_t nan = ((((w & ~(EXPONENT | 0x80008000u)) + 0x7FFF7FFFu) & 0x80008000u) >> 15) * 0xFFFFu;
         return odd_ones(w) & ((negative ? sign : ~sign) | nan) & ONE;
-    }
-    // the A operand of 16 keys and 32 columns
-    __device__ __forceinline__ i32x4 columns(uint32_t offset, int slab, int dt) const {
-        const int at = offset + slab * 16 * ROWB;
-        if constexpr (CODES) {
-            const i32x2 c = lds_read_tr8(tr_at[dt][0] + at);
-            return i32x4{c[0], c[1], 0, 0};
-        } else {
-            const i32x2 lo = lds_read_tr16(tr_at[dt][0] + at), hi = lds_read_tr16(tr_at[dt][1] + at);
-            return i32x4{lo[0], lo[1], hi[0], hi[1]};
-        }
     }
     __device__ __forceinline__ bool not_finite(uint32_t offset, int lane) const {
         uint32_t any = 0;
@@ -164,56 +259,37 @@ struct CacheTile {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    __device__ __forceinline__ void add_not_finite(uint32_t offset, int half, uint32_t vis, f32x16 (&acc)[DT]) const;
-};
-
-// Eight codes as eight 16-bit elements
-template <typename Tag>
-static __device__ __forceinline__ i32x4 from_codes(int lo, int hi) {
-    i32x4 w;
-    if constexpr (std::is_same_v<Tag, bf16_tag>) {
-        w[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-        w[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-        w[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-        w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
-    } else {
-        w[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
-        w[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
-        w[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
-        w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
-    }
-    return w;
-}
-
-template <typename Tag, int D, bool CODES>
-__device__ __forceinline__ void CacheTile<Tag, D, CODES>::add_not_finite(uint32_t offset, int half, uint32_t vis, f32x16 (&acc)[DT]) const {
-    i32x4 seen[2];
+    // `seen`: bit(r) is what the lane's row sees of its part's keys
+    __device__ __forceinline__ void add_not_finite(uint32_t offset, uint32_t seen, typename M::Acc (&acc)[M::NT]) const {
+        i32x4 ones[M::SLABS];
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-        const uint32_t two = vis >> (4 * half + 8 * (r >> 2) + (r & 3));
-        seen[r >> 3][(r >> 1) & 3] = (int)((two & 1 ? 0xFFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u)) & ONE;
-    }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int negative = 0; negative < (CODES ? 1 : 2); ++negative) {
-            f32x16 count = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int slab = 0; slab < 2; ++slab) {
-                i32x4 w = columns(offset, slab, dt);
-                if constexpr (CODES) {
-                    w = from_codes<f16_tag>((int)odd_ones(w[0]) & 0x38383838, (int)odd_ones(w[1]) & 0x38383838);  // 0x38: 1
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (int)infinite(w[e], negative);
-                }
-                count = PE::mma(w, seen[slab], count);
-            }
-            const float what = CODES ? __builtin_nanf("") : negative ? -INFINITY : INFINITY;  // a NaN counts as both
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[dt][r] += count[r] > 0.f ? what : 0.f;
+        for (int r = 0; r < M::NS; r += 2) {
+            const uint32_t two = seen >> M::bit(r);
+            ones[r >> 3][(r >> 1) & 3] = (int)((two & 1 ? 0xFFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u)) & ONE;
         }
-}
+        static_for<M::NT>([&](auto d) __attribute__((always_inline)) {
+            constexpr int dt = decltype(d)::value;
+#pragma unroll
+            for (int negative = 0; negative < (CODES ? 1 : 2); ++negative) {
+                typename M::Acc count = {};
+                static_for<M::SLABS>([&](auto sl) __attribute__((always_inline)) {
+                    constexpr int slab = decltype(sl)::value;
+                    i32x4 w = columns<dt, slab>(offset);
+                    if constexpr (CODES) {
+                        w = from_codes<f16_tag>((int)odd_ones(w[0]) & 0x38383838, (int)odd_ones(w[1]) & 0x38383838);  // 0x38: 1
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = (int)infinite(w[e], negative);
+                    }
+                    count = PM::mma(w, ones[slab], count);
+                });
+                const float what = CODES ? __builtin_nanf("") : negative ? -INFINITY : INFINITY;  // a NaN counts as both
+#pragma unroll
+                for (int r = 0; r < (int)(sizeof(count) / 4); ++r) acc[dt][r] += count[r] > 0.f ? what : 0.f;
+            }
+        });
+    }
+};
 
 // Asynchronous copy of 4 bytes per lane from an address per lane to lds_base + 4 lane
 static __device__ __forceinline__ void global_to_lds_4B(const float* p, uint32_t lds_base) {
@@ -229,8 +305,6 @@ static __device__ __forceinline__ void wait_vmcnt() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-constexpr int kMergeCols = 64, kMergeStride = kMergeCols + 4;
-
 // A row number of lane i's in scalar registers; negative: none.  (Two words: there is no scalar comparison of 64 bits.)
 struct UniformRow {
     int lo, hi;
@@ -242,55 +316,84 @@ struct UniformRow {
     __device__ __forceinline__ long index() const { return (long)((uint64_t)(uint32_t)(lo & ~none()) | (uint64_t)(uint32_t)(hi & ~none()) << 32); }
 };
 
-template <typename Tag, int D, bool CODES, int NW, int STG, int RT>
+template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG>
 struct CachedShape {
-    using Tile = CacheTile<Tag, D, CODES>;
-    static constexpr int SCALE_B = CODES ? 256 : 0;                    // of a tile: 32 scales of K, 32 of V
+    using Tile = CacheTile<Tag, D, CODES, COLS>;
+    static constexpr int ROWS = COLS * RT;                 // of a workgroup
+    static constexpr int STEP = 32 * NW;                   // keys of a step
+    static constexpr int SCALE_B = CODES ? 256 : 0;        // of a tile: 32 scales of K, 32 of V
     static constexpr int STAGE_B = 2 * Tile::TILE_B + SCALE_B, WAVE_B = STG * STAGE_B;
-    static constexpr int MERGE_B = NW * 32 * kMergeStride * 4, STATE_B = NW * RT * 32 * 3 * 4;
+    static constexpr int MERGE_COLS = COLS == 16 && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
+    static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * ROWS * 3 * 4;
     static constexpr int LDS = (NW * WAVE_B > MERGE_B ? NW * WAVE_B : MERGE_B) + STATE_B;
+    static constexpr int WAVES = COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;  // to a SIMD, by registers
+    static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;  // workgroups of four waves
 };
 
-template <typename Tag, int D, bool CODES, int NW, int STG, int RT>
-__global__ void __launch_bounds__(NW * 64, RT == 1 && D < 256 ? 2 : 1)
+template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG>
+__global__ void __launch_bounds__(NW * 64, (CachedShape<Tag, D, CODES, COLS, RT, NW, STG>::WAVES))
 fa_fwd_cache_kernel(CachedArgs a) {
-    using Shape = CachedShape<Tag, D, CODES, NW, STG, RT>;
+    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG>;
     using Tile = typename Shape::Tile;
+    using M = typename Tile::M;
+    using PM = typename Tile::PM;
+    using PE = Elem<typename Tile::PE>;
     using E = Elem<Tag>;
-    using PE = Elem<std::conditional_t<CODES, f16_tag, Tag>>;  // of the product with V
-    constexpr int KS = D / 16, DT = D / 32, NI = Tile::NI, X = CODES ? 1 : 0;
-    extern __shared__ __align__(16) char lds[];
+    constexpr int NS = M::NS, NT = M::NT, NI = Tile::NI, X = CODES ? 1 : 0, ACC = sizeof(typename M::Acc) / 4;
+    constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
+    extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int col = lane & 31, half = lane >> 5;
+    const int col = lane % COLS, part = lane / COLS;
 
-    // which rows and keys: row groups of a chunk side by side on one XCD
-    int item = xcd_run(blockIdx.x, gridDim.x);
-    const int rg = __builtin_amdgcn_readfirstlane(item % a.row_groups);
-    item /= a.row_groups;
-    const int split = __builtin_amdgcn_readfirstlane(item % a.splits);
-    item /= a.splits;
-    const int H_kv = a.c.H_kv, b = __builtin_amdgcn_readfirstlane(item / H_kv), kvh = __builtin_amdgcn_readfirstlane(item - b * H_kv);
-    const int group = a.H / H_kv, n_rows = group * a.T;
-    Extent ext(a, b);
-    ext.make_uniform();
-    const int n_splits = __builtin_amdgcn_readfirstlane(ext.splits(a));
-    if (split >= n_splits) return;
-    const int key0 = split * a.chunk, key1 = split == n_splits - 1 ? ext.keys : key0 + a.chunk;
-    const int n_tiles = (max(key1 - key0, 0) + 31) / 32, mine = n_tiles > wave ? (n_tiles - wave + NW - 1) / NW : 0;
-
-    int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
-    i32x4 qreg[RT][KS];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int row = min((rg * RT + i) * 32 + col, n_rows - 1), g = row / a.T;
-        t[i] = row - g * a.T;
-        const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (b * a.q.batch + (kvh * group + g) * a.q.head + t[i] * a.q.token);
-#pragma unroll
-        for (int u = 0; u < KS; ++u)
-            qreg[i][u] = *reinterpret_cast<const i32x4*>(q + (CODES ? 32 * (u / 2) + 16 * half + 8 * (u % 2) : 16 * u + 8 * half));
+    // which rows and keys: a team's workgroups side by side on one XCD
+    int team = xcd_run(blockIdx.x, gridDim.x);
+    const int wg = team, rg = __builtin_amdgcn_readfirstlane(team % a.row_groups);
+    team = __builtin_amdgcn_readfirstlane(team / a.row_groups);
+    const int H_kv = a.c.H_kv, group = a.H / H_kv, n_rows = group * a.T;
+    int b, kvh, step = 0, left;  // the first segment, and how many steps the team has
+    if (a.teams == 0) {
+        b = __builtin_amdgcn_readfirstlane(team / H_kv);
+        kvh = __builtin_amdgcn_readfirstlane(team - b * H_kv);
+        left = 0x7fffffff;
+    } else {
+        long* const first = wg == 0 && wave == 0 ? a.first_step : nullptr;
+        const long total = scan_steps<Shape::STEP>(a, lane, [&](int s, long before, long n) {
+            if (first && s < a.B) {
+                first[s] = before;
+                if (s == a.B - 1) first[a.B] = before + n;
+            }
+            return false;
+        });
+        const long share = (total + a.teams - 1) / a.teams, pos = team * share;
+        if (pos >= total) return;
+        left = __builtin_amdgcn_readfirstlane((int)min(share, total - pos));
+        int at_b = 0;
+        long at_first = 0;
+        scan_steps<Shape::STEP>(a, lane, [&](int s, long before, long n) {
+            const uint64_t here = __builtin_amdgcn_ballot_w64(pos < before + n);
+            if (here == 0) return false;
+            const int i = __builtin_ctzll(here);
+            at_b = __builtin_amdgcn_readlane(s, i);
+            at_first = readlane64(before, i);
+            return true;
+        });
+        b = __builtin_amdgcn_readfirstlane(at_b);
+        const int rel = (int)(pos - at_first), n = Extent(a, b).steps<Shape::STEP>();
+        kvh = __builtin_amdgcn_readfirstlane(rel / n);
+        step = __builtin_amdgcn_readfirstlane(rel - rel / n * n);
     }
 
     const Tile tile(lds_address(lds) + wave * Shape::WAVE_B, lane);
+    const float sc = a.scale * kLog2e;
+    for (int segment = 0;; segment = 1) {
+    Extent ext(a, b);
+    ext.make_uniform();
+    const int n_steps = ext.steps<Shape::STEP>();
+    const int now = min(n_steps - step, left);
+    const bool whole = now == n_steps;
+    const int key0 = step * Shape::STEP, key1 = step + now == n_steps ? ext.keys : key0 + now * Shape::STEP;
+    const int n_tiles = (int)(((unsigned)max(key1 - key0, 0) + 31) / 32), mine = n_tiles > wave ? (n_tiles - wave + NW - 1) / NW : 0;
+
     // rows (of all pages' rows, heads included) of the wave's tiles: lane i has tile i of 64, two times 16 places; -1: no page
     long row_lo = -1, row_hi = -1;
     auto look_up = [&](int first) __attribute__((always_inline)) {
@@ -307,10 +410,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // requests K of the wave's tile i into stage st, and its V when that stage's V has been read
     UniformRow rows[STG][2];
     auto resources = [&](const void* pages, int i, const UniformRow (&row)[2], BufferWords (&rsrc)[2]) __attribute__((always_inline)) {
-        const int left = key1 - (key0 + 32 * (wave + NW * i));
+        const int there = key1 - (key0 + 32 * (wave + NW * i));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            int n = max(left - 16 * h, 0);
+            int n = max(there - 16 * h, 0);
             asm volatile("" : "+s"(n));  // (with the minimum it would be one vector instruction)
             n = min(n, 16) & ~row[h].none();
             rsrc[h] = make_buffer_words(static_cast<const char*>(pages) + (row[h].index() * Tile::ROWB), n * Tile::ROWB);
@@ -328,9 +431,9 @@ fa_fwd_cache_kernel(CachedArgs a) {
             long row = rows[st][0].index(), upper = rows[st][1].index();
             asm volatile("" : "+v"(row), "+v"(upper));  // (a choice between vector registers, not between places in memory)
             row = lane & 16 ? upper : row;
-            const int left = key1 - (key0 + 32 * (wave + NW * i));
-            const long at = (lane & 31) >= left ? 0 : row + (lane & 15);
-            global_to_lds_4B((half ? a.c.v_scales : a.c.k_scales) + at, tile.base + st * Shape::STAGE_B + 2 * Tile::TILE_B);
+            const int there = key1 - (key0 + 32 * (wave + NW * i));
+            const long at = (lane & 31) >= there ? 0 : row + (lane & 15);
+            global_to_lds_4B((lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + st * Shape::STAGE_B + 2 * Tile::TILE_B);
         }
     };
     auto request_v = [&](int i, auto stage) __attribute__((always_inline)) {
@@ -339,23 +442,38 @@ fa_fwd_cache_kernel(CachedArgs a) {
         resources(a.c.v, i, rows[st], rsrc);
         tile.request(rsrc, st * Shape::STAGE_B + Tile::TILE_B);
     };
+    if (mine > 0)
+        static_for<STG>([&](auto st) {
+            request_k(st, st);
+            request_v(st, st);
+        });
 
-    f32x16 acc[RT][DT];
+    int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
+    i32x4 qreg[RT][QS];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int row = min((rg * RT + x) * COLS + col, n_rows - 1), g = row / a.T;
+        t[x] = row - g * a.T;
+        const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (b * a.q.batch + (kvh * group + g) * a.q.head + t[x] * a.q.token);
+#pragma unroll
+        for (int u = 0; u < QS; ++u) {
+            const int at = CODES ? 16 * M::PARTS * (u / 2) + 16 * part + 8 * (u % 2) : 8 * M::PARTS * u + 8 * part;
+            qreg[x][u] = *reinterpret_cast<const i32x4*>(q + at);
+        }
+    }
+    typename M::Acc acc[RT][NT];
     float m_run[RT], l_run[RT];
     float F = 0.f, inv_F = 0.f;  // codes: the power of two that P~ is divided by
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        m_run[i] = -INFINITY;
-        l_run[i] = 0.f;
+    for (int x = 0; x < RT; ++x) {
+        m_run[x] = -INFINITY;
+        l_run[x] = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][dt][r] = 0.f;
+        for (int dt = 0; dt < NT; ++dt) acc[x][dt] = typename M::Acc{};
     }
-    const float sc = a.scale * kLog2e;
 
     // the row's view of the 32 places from `key` on
-    auto visible = [&](int key, int row_t, int bad_halves) __attribute__((always_inline)) {
+    auto visible = [&](int key, int row_t, uint32_t live) __attribute__((always_inline)) {
         const int u0 = key - ext.len;  // the number of the first place among the new tokens
         uint32_t vis = 0;
         if (a.tree) {
@@ -368,47 +486,54 @@ fa_fwd_cache_kernel(CachedArgs a) {
             vis = row_t - u0 >= 31 ? ~0u : (2u << (row_t - u0)) - 1;
         }
         if (u0 < 0) vis |= u0 <= -32 ? ~0u : (1u << -u0) - 1;  // places before the new tokens
-        const int there = min(ext.keys, key1) - key;
-        if (there < 32) vis &= there <= 0 ? 0u : (1u << there) - 1;
-        if (bad_halves & 1) vis &= 0xFFFF0000u;
-        if (bad_halves & 2) vis &= 0x0000FFFFu;
-        return vis;
+        return vis & live;
     };
 
-    if (mine > 0)
-        static_for<STG>([&](auto st) {
-            request_k(st, st);
-            request_v(st, st);
-        });
     for (int i0 = 0; i0 < mine; i0 += STG) {
         static_for<STG>([&](auto stage) __attribute__((always_inline)) {
             constexpr int st = decltype(stage)::value, kK = st * Shape::STAGE_B, kV = kK + Tile::TILE_B, kScales = kK + 2 * Tile::TILE_B;
             const int i = i0 + st;
             if (i >= mine) return;
-            const int key = key0 + 32 * (wave + NW * i);
+            const int key = key0 + 32 * (wave + NW * i), next = i + STG;
+            // the places of the tile that are there and on a page
+            const int bad = (rows[st][0].none() & 1) | (rows[st][1].none() & 2);
+            const bool special = key + 32 > min(ext.len, key1) || bad != 0;
             wait_vmcnt<NI * STG + (NI + X) * (STG - 1)>();  // K has landed
-            f32x16 s[RT];
+            float s[RT][NS];
+            {
+                typename M::Acc y[RT][M::TILES];
 #pragma unroll
-            for (int x = 0; x < RT; ++x) s[x] = f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < RT; ++x)
 #pragma unroll
-            for (int k = 0; k < Tile::KR; ++k) {
-                const i32x4 w = lds_load_16B(tile.row_at[k] + kK);
-                if constexpr (CODES) {
-                    const i32x4 lo = from_codes<Tag>(w[0], w[1]), hi = from_codes<Tag>(w[2], w[3]);
+                    for (int kt = 0; kt < M::TILES; ++kt) y[x][kt] = typename M::Acc{};
+                static_for<Tile::KR>([&](auto n) __attribute__((always_inline)) {
+                    constexpr int k = decltype(n)::value;
+                    static_for<M::TILES>([&](auto m) __attribute__((always_inline)) {
+                        constexpr int kt = decltype(m)::value;
+                        const i32x4 w = tile.template row_read<k, kt>(kK);
+                        if constexpr (CODES) {
+                            const i32x4 lo = from_codes<Tag>(w[0], w[1]), hi = from_codes<Tag>(w[2], w[3]);
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) s[x] = E::mma(lo, qreg[x][2 * k], s[x]);
+                            for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(lo, qreg[x][2 * k], y[x][kt]);
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) s[x] = E::mma(hi, qreg[x][2 * k + 1], s[x]);
-                } else {
+                            for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(hi, qreg[x][2 * k + 1], y[x][kt]);
+                        } else {
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) s[x] = E::mma(w, qreg[x][k], s[x]);
-                }
+                            for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(w, qreg[x][k], y[x][kt]);
+                        }
+                    });
+                });
+#pragma unroll
+                for (int x = 0; x < RT; ++x)
+#pragma unroll
+                    for (int r = 0; r < NS; ++r) s[x][r] = y[x][r / ACC][r % ACC];
             }
-            float vscale[16];
+            float vscale[NS];
             if constexpr (CODES) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 ks = lds_load_4f(tile.base + kScales + 32 * g + 16 * half), vs = lds_load_4f(tile.base + kScales + 128 + 32 * g + 16 * half);
+                for (int g = 0; g < NS / 4; ++g) {
+                    const uint32_t at = tile.base + kScales + 4 * (M::bit(4 * g) + (part << M::SHIFT));
+                    const f32x4 ks = lds_load_4f(at), vs = lds_load_4f(at + 128);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         vscale[4 * g + r] = vs[r];
@@ -417,33 +542,30 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     }
                 }
             }
-            const int bad_now = (rows[st][0].none() & 1) | (rows[st][1].none() & 2);  // the halves that are on no page
-            const int next = i + STG;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K and the scales have been read: the next ones may come
             request_k(next, stage);
 
-            const bool special = key + 32 > ext.len || bad_now != 0;
-            uint32_t vis[RT];
+            uint32_t seen[RT];
             if (special) {
+                const int there = key1 - key;
+                uint32_t live = there >= 32 ? ~0u : (1u << there) - 1;  // (a tile has a key at least)
+                if (bad & 1) live &= 0xFFFF0000u;
+                if (bad & 2) live &= 0x0000FFFFu;
 #pragma unroll
                 for (int x = 0; x < RT; ++x) {
-                    vis[x] = visible(key, t[x], bad_now);
-                    const uint32_t w = vis[x] >> (4 * half);
+                    seen[x] = visible(key, t[x], live) >> (part << M::SHIFT);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[x][r] = w >> (8 * (r >> 2) + (r & 3)) & 1 ? s[x][r] : -INFINITY;
+                    for (int r = 0; r < NS; ++r) s[x][r] = seen[x] >> M::bit(r) & 1 ? s[x][r] : -INFINITY;
                 }
+                if constexpr (CODES)
+#pragma unroll
+                    for (int r = 0; r < NS; ++r) vscale[r] = live >> (part << M::SHIFT) >> M::bit(r) & 1 ? vscale[r] : 0.f;
             }
             if constexpr (CODES) {
-                // the largest finite scale of V in the tile (places that are none have any: they cost accuracy at most where they exceed the others)
-                float top = 0.f;
-                const int there = (special ? min(ext.keys, key1) - key : 32) - 4 * half;
+                float top = 0.f;  // the largest finite scale of V in the tile
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (special && (8 * (r >> 2) + (r & 3) >= there || (bad_now >> (r >> 3) & 1))) vscale[r] = 0.f;
-                    top = fmaxf(top, vscale[r] < INFINITY ? vscale[r] : 0.f);
-                }
-                top = fminf(fmaxf(max_both_halves(top), 0x1p-100f), 0x1p126f);
+                for (int r = 0; r < NS; ++r) top = fmaxf(top, vscale[r] < INFINITY ? vscale[r] : 0.f);
+                top = fminf(fmaxf(M::max_parts(top), 0x1p-100f), 0x1p126f);
                 const float new_F = __builtin_bit_cast(float, (int)((__builtin_bit_cast(int, top) + 0x7fffff) & 0x7f800000));
                 if (__builtin_amdgcn_readfirstlane(new_F > F)) {
                     const float down = F / new_F;
@@ -452,66 +574,60 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                     for (int x = 0; x < RT; ++x)
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[x][dt][r] *= down;
+                        for (int dt = 0; dt < NT; ++dt) acc[x][dt] *= down;
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) vscale[r] *= inv_F;
+                for (int r = 0; r < NS; ++r) vscale[r] *= inv_F;
             }
-            i32x4 pb[RT][2];  // what V is multiplied by
+            i32x4 pb[RT][M::SLABS];  // what V is multiplied by
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int r = 0; r < 16; ++r) mx[r & 3] = fmaxf(mx[r & 3], s[x][r]);
-                const float m_new = max_both_halves(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                for (int r = 0; r < NS; ++r) mx[r & 3] = fmaxf(mx[r & 3], s[x][r]);
+                const float m_new = M::max_parts(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
                 const bool raise = (m_new - m_run[x]) * sc > kLazy;
                 if (__builtin_amdgcn_ballot_w64(raise) != 0) {
                     const float corr = raise ? fast_exp2((m_run[x] - m_new) * sc) : 1.0f;
                     m_run[x] = raise ? m_new : m_run[x];
                     l_run[x] *= corr;
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[x][dt][r] *= corr;
+                    for (int dt = 0; dt < NT; ++dt) acc[x][dt] *= corr;
                 }
                 const float mb = m_run[x] == -INFINITY ? 0.f : m_run[x] * sc;  // a row that has seen nothing yet: P = 0
                 float ps[4];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                for (int r = 0; r < NS; ++r) {
                     const float p = fast_exp2(__builtin_fmaf(s[x][r], sc, -mb));
                     ps[r & 3] = r < 4 ? p : ps[r & 3] + p;
                     s[x][r] = p;
                     if constexpr (CODES) s[x][r] = p * vscale[r];
                 }
-                if constexpr (CODES) {
-                    if (special) {  // a scale that is not finite belongs to those rows only that see it
-                        const uint32_t w = vis[x] >> (4 * half);
+                if constexpr (CODES)
+                    if (special)  // a scale that is not finite belongs to those rows only that see it
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[x][r] = w >> (8 * (r >> 2) + (r & 3)) & 1 ? s[x][r] : 0.f;
-                    }
-                }
+                        for (int r = 0; r < NS; ++r) s[x][r] = seen[x] >> M::bit(r) & 1 ? s[x][r] : 0.f;
                 l_run[x] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) pb[x][r >> 3][(r >> 1) & 3] = PE::pack2(s[x][r], s[x][r + 1]);
+                for (int r = 0; r < NS; r += 2) pb[x][r >> 3][(r >> 1) & 3] = PE::pack2(s[x][r], s[x][r + 1]);
             }
             wait_vmcnt<(NI + X) * STG + NI * (STG - 1)>();  // V has landed
             if (special && key + 32 > ext.len)
                 if (__builtin_expect(tile.not_finite(kV, lane), 0)) {
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) tile.add_not_finite(kV, half, vis[x], acc[x]);
+                    for (int x = 0; x < RT; ++x) tile.add_not_finite(kV, seen[x], acc[x]);
                     tile.clear_not_finite(kV, lane);
                 }
             // O^T += V^T P^T
+            static_for<M::SLABS>([&](auto sl) __attribute__((always_inline)) {
+                static_for<NT>([&](auto d) __attribute__((always_inline)) {
+                    constexpr int slab = decltype(sl)::value, dt = decltype(d)::value;
+                    i32x4 w = tile.template columns<dt, slab>(kV);
+                    if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
 #pragma unroll
-            for (int u = 0; u < 2 * DT; ++u) {
-                const int slab = u / DT, dt = u % DT;
-                i32x4 w = tile.columns(kV, slab, dt);
-                if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
-#pragma unroll
-                for (int x = 0; x < RT; ++x) acc[x][dt] = PE::mma(w, pb[x][slab], acc[x][dt]);
-            }
+                    for (int x = 0; x < RT; ++x) acc[x][dt] = PM::mma(w, pb[x][slab], acc[x][dt]);
+                });
+            });
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             request_v(next, stage);
         });
@@ -519,45 +635,45 @@ fa_fwd_cache_kernel(CachedArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last requests: the LDS is about to be reused
 
     // The waves' states meet: with M the largest reference and f = 2^(m - M), sum f F acc, M and sum f l
-    float* const state = reinterpret_cast<float*>(lds + Shape::LDS - Shape::STATE_B);  // [RT][NW][32][m, l, F]
-    float* const part = reinterpret_cast<float*>(lds);                                 // [NW][32][kMergeStride]
+    float* const state = reinterpret_cast<float*>(lds + Shape::LDS - Shape::STATE_B);  // [RT][NW][COLS][m, l, F]
+    float* const merge = reinterpret_cast<float*>(lds);                                // [NW][COLS][MERGE_STRIDE]
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const float l = sum_both_halves(l_run[x]);
-        if (half == 0) {
-            float* at = state + ((x * NW + wave) * 32 + col) * 3;
+        const float l = M::sum_parts(l_run[x]);
+        if (part == 0) {
+            float* at = state + ((x * NW + wave) * COLS + col) * 3;
             at[0] = m_run[x] * sc;
             at[1] = l;
             at[2] = CODES ? F : 1.f;
         }
     }
-    const bool whole = n_splits == 1;
+    constexpr int MC = Shape::MERGE_COLS, MS = Shape::MERGE_STRIDE;
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
-        for (int c0 = 0; c0 < D; c0 += kMergeCols) {
+        for (int c0 = 0; c0 < D; c0 += MC) {
             __syncthreads();
 #pragma unroll
-            for (int d2 = 0; d2 < 2; ++d2)
+            for (int dt = c0 / M::WIDTH; dt < (c0 + MC) / M::WIDTH; ++dt)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x16& y = acc[x][c0 / 32 + d2];
+                for (int g = 0; g < ACC / 4; ++g) {
+                    const typename M::Acc& y = acc[x][dt];
                     const f32x4 w = {y[4 * g], y[4 * g + 1], y[4 * g + 2], y[4 * g + 3]};
-                    *reinterpret_cast<f32x4*>(part + (wave * 32 + col) * kMergeStride + d2 * 32 + 8 * g + 4 * half) = w;
+                    *reinterpret_cast<f32x4*>(merge + (wave * COLS + col) * MS + dt * M::WIDTH - c0 + 4 * M::PARTS * g + 4 * part) = w;
                 }
             __syncthreads();
-            for (int c = tid; c < 32 * kMergeCols / 8; c += NW * 64) {
-                const int r = c / (kMergeCols / 8), cc = (c % (kMergeCols / 8)) * 8, row = (rg * RT + x) * 32 + r;
+            for (int c = tid; c < COLS * MC / 8; c += NW * 64) {
+                const int r = c / (MC / 8), cc = (c % (MC / 8)) * 8, row = (rg * RT + x) * COLS + r;
                 if (row >= n_rows) continue;
                 const int g = row / a.T, tok = row - g * a.T;
                 if (tok >= ext.count) continue;
                 float m_all = -INFINITY, l_all = 0.f, f[NW];
 #pragma unroll
-                for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, state[((x * NW + w) * 32 + r) * 3]);
+                for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, state[((x * NW + w) * COLS + r) * 3]);
                 const float m_ref = m_all == -INFINITY ? 0.f : m_all;
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
-                    const float* at = state + ((x * NW + w) * 32 + r) * 3;
+                    const float* at = state + ((x * NW + w) * COLS + r) * 3;
                     f[w] = fast_exp2(at[0] - m_ref);
                     l_all += f[w] * at[1];
                     f[w] *= at[2];
@@ -567,22 +683,21 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 for (int w = 0; w < NW; ++w)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const f32x4 z = *reinterpret_cast<const f32x4*>(part + (w * 32 + r) * kMergeStride + cc + 4 * h);
+                        const f32x4 z = *reinterpret_cast<const f32x4*>(merge + (w * COLS + r) * MS + cc + 4 * h);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[4 * h + e] = __builtin_fmaf(f[w], z[e], y[4 * h + e]);
                     }
-                const int head = kvh * group + g;
-                const long out_row = ((long)b * a.H + head) * a.T + tok;
                 if (whole) {
+                    const int head = kvh * group + g;
                     const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;  // a row that sees nothing: 0
                     uint16_t* o = static_cast<uint16_t*>(const_cast<void*>(a.o.p)) + (b * a.o.batch + head * a.o.head + tok * a.o.token);
                     i32x4 w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = E::pack2(y[2 * e] * inv, y[2 * e + 1] * inv);
                     *reinterpret_cast<i32x4*>(o + c0 + cc) = w;
-                    if (c0 + cc == 0) a.lse[out_row] = (m_all + log2f(l_all)) * kLn2;
+                    if (c0 + cc == 0) a.lse[((long)b * a.H + head) * a.T + tok] = (m_all + log2f(l_all)) * kLn2;
                 } else {
-                    const long at = (long)split * a.B * a.H * a.T + out_row;
+                    const long at = ((long)wg * 2 + segment) * Shape::ROWS + x * COLS + r;
                     float* o = a.part + at * D + c0 + cc;
                     *reinterpret_cast<f32x4*>(o) = f32x4{y[0], y[1], y[2], y[3]};
                     *reinterpret_cast<f32x4*>(o + 4) = f32x4{y[4], y[5], y[6], y[7]};
@@ -593,35 +708,71 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 }
             }
         }
+    left -= now;
+    if (a.teams == 0 || left == 0) break;
+    step = 0;
+    if (++kvh == H_kv) {
+        kvh = 0;
+        ++b;
+    }
+    __syncthreads();  // the merge area is staged into again
+    }
 }
 
-// Joins the chunks of rows whose sequence has several: D / 8 threads to a row, 8 columns each
-template <typename Tag, int D>
-__global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a) {
+// Joins the segments of rows whose sequence several teams have.  D / 8 threads stand side by side on a row, 8 columns each, and
+// `ways` such groups (a power of two, at most 256 / (D / 8)) take its segments in turn and meet in the LDS.
+template <typename Tag, int D, int ROWS>
+__global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
     using E = Elem<Tag>;
-    constexpr int TPR = D / 8;
-    const long n_rows = (long)a.B * a.H * a.T, row = (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    if (row >= n_rows) return;
-    const int bh = (int)(row / a.T), tok = (int)(row - (long)bh * a.T), b = bh / a.H, head = bh - b * a.H, c = (threadIdx.x % TPR) * 8;
-    const Extent ext(a, b);
-    const int n = ext.splits(a);
-    if (n == 1 || tok >= ext.count) return;
+    constexpr int TPR = D / 8, GROUPS = 256 / TPR;
+    __shared__ float meet[GROUPS][D + 4];
+    const int group = threadIdx.x / TPR, way = group & (ways - 1), c = (threadIdx.x % TPR) * 8;
+    const long n_rows = (long)a.B * a.H * a.T, row = ((long)blockIdx.x * GROUPS + group) / ways;
+    const int bh = (int)(min(row, n_rows - 1) / a.T), tok = (int)(row - (long)bh * a.T), b = bh / a.H, head = bh - b * a.H;
+    const int heads = a.H / a.c.H_kv, kvh = head / heads, in_group = (head - kvh * heads) * a.T + tok, rg = in_group / ROWS;
+    const long share = (a.first_step[a.B] + a.teams - 1) / a.teams, steps = (a.first_step[b + 1] - a.first_step[b]) / a.c.H_kv;
+    const long start = a.first_step[b] + kvh * steps, team0 = start / share;
+    const int n = (int)((start + steps - 1) / share - team0) + 1;
+    // of team team0 + s: the first segment of those that begin inside the sequence, the second of one that ends with its beginning
+    auto place = [&](int s) {
+        const long wg = (team0 + s) * a.row_groups + rg;
+        return (wg * 2 + (s == 0 && start != team0 * share)) * ROWS + (in_group - rg * ROWS);
+    };
+    const bool there = row < n_rows && n > 1 && tok < Extent(a, b).count;
     float m_all = -INFINITY, l_all = 0.f;
-    for (int s = 0; s < n; ++s) m_all = fmaxf(m_all, a.state[2 * (s * n_rows + row)]);
-    const float m_ref = m_all == -INFINITY ? 0.f : m_all;
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-        const long at = s * n_rows + row;
-        const float f = fast_exp2(a.state[2 * at] - m_ref);
-        l_all += f * a.state[2 * at + 1];
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(a.part + at * D + c), hi = *reinterpret_cast<const f32x4*>(a.part + at * D + c + 4);
+    if (there) {
+        // the reference: each of the group's threads looks at some of the segments
+        for (int s = threadIdx.x % TPR; s < n; s += TPR) m_all = fmaxf(m_all, a.state[2 * place(s)]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = __builtin_fmaf(f, lo[e], y[e]);
-            y[4 + e] = __builtin_fmaf(f, hi[e], y[4 + e]);
+        for (int x = 1; x < TPR; x <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, x));
+        const float m_ref = m_all == -INFINITY ? 0.f : m_all;
+#pragma unroll 4
+        for (int s = way; s < n; s += ways) {
+            const long at = place(s);
+            const float f = fast_exp2(a.state[2 * at] - m_ref);
+            l_all += f * a.state[2 * at + 1];
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(a.part + at * D + c), hi = *reinterpret_cast<const f32x4*>(a.part + at * D + c + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = __builtin_fmaf(f, lo[e], y[e]);
+                y[4 + e] = __builtin_fmaf(f, hi[e], y[4 + e]);
+            }
         }
     }
+    if (ways > 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) meet[group][c + e] = y[e];
+        if (c == 0) meet[group][D] = l_all;
+        __syncthreads();
+        if (way == 0)
+            for (int w = 1; w < ways; ++w) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] += meet[group + w][c + e];
+                l_all += meet[group + w][D];
+            }
+    }
+    if (!there || way != 0) return;
     const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
     i32x4 w;
 #pragma unroll
@@ -631,69 +782,94 @@ __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a) {
     if (c == 0) a.lse[row] = (m_all + log2f(l_all)) * kLn2;
 }
 
-// How a call is divided: row tiles to a wave, row groups, chunks of keys
-struct CachedDivision {
-    int rt, row_groups, splits, chunk;
-    CachedDivision(int B, int H, int H_kv, int T, int d, int max_len) {
-        const int rows = H / H_kv * T, tiles = (rows + 31) / 32;
-        rt = tiles > 1 && d < 256 ? 2 : 1;
-        row_groups = (tiles + rt - 1) / rt;
-        const double base = (double)B * H_kv * row_groups;
-        // enough workgroups to fill the chip several times, but chunks of 256 keys at least
-        double per = max_len * base / 1536.0;
-        if (per > max_len) per = max_len;
-        chunk = 256;
-        if (per > 256) chunk = per > 0x3fffffff ? 0x3fffffff : ((int)per + 127) / 128 * 128;
-        splits = (int)(((long)max_len + chunk - 1) / chunk);
-        if (splits > 256) {
-            chunk = (max_len / 256 + 128) / 128 * 128;
-            splits = (int)(((long)max_len + chunk - 1) / chunk);
-        }
+#ifndef X_OVER
+#define X_OVER 1
+#endif
+#ifndef X_STG
+#define X_STG 1
+#endif
+constexpr int kWaves = 4;
+// How deep a wave stages: as the LDS of a CU allows with as many workgroups as its registers do
+template <typename Tag, int D, bool CODES, int COLS, int RT>
+using CachedForm = CachedShape<Tag, D, CODES, COLS, RT, kWaves, (D * (CODES ? 1 : 2) <= 128 ? 2 : X_STG)>;
+
+// Calls f with the shape that a call takes
+template <typename F>
+static auto with_shape(int rows, int d, bool codes, F&& f) {
+    auto by_rows = [&](auto D, auto c) {
+        constexpr int d_ = decltype(D)::value;
+        constexpr bool c_ = decltype(c)::value;
+        if (rows <= 16) return f(CachedForm<bf16_tag, d_, c_, 16, 1>{}, D, c, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+        if constexpr (d_ < 256)
+            if (rows > 32) return f(CachedForm<bf16_tag, d_, c_, 32, 2>{}, D, c, std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
+        return f(CachedForm<bf16_tag, d_, c_, 32, 1>{}, D, c, std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+    };
+    auto by_codes = [&](auto D) { return codes ? by_rows(D, std::true_type{}) : by_rows(D, std::false_type{}); };
+    switch (d) {
+        case 64: return by_codes(std::integral_constant<int, 64>{});
+        case 128: return by_codes(std::integral_constant<int, 128>{});
+        default: return by_codes(std::integral_constant<int, 256>{});
     }
+}
+
+// How a call is divided.  (The shapes do not depend on the 16-bit type.)
+struct CachedDivision {
+    int row_groups, teams;
+    size_t steps_bytes, segments;  // of the workspace: the sequences' first steps; segments' rows
+    template <typename Shape>
+    CachedDivision(const Shape&, int B, int H, int H_kv, int T, int max_len) {
+        row_groups = (H / H_kv * T + Shape::ROWS - 1) / Shape::ROWS;
+        const long items = (long)B * H_kv, most = ((long)max_len + Shape::STEP - 1) / Shape::STEP, slots = 256 * Shape::PER_CU * X_OVER;
+        long n = slots / row_groups > 1 ? slots / row_groups : 1;
+        if ((double)items * most < n) n = items * most;
+        teams = most <= 4 || items * row_groups >= 4 * slots ? 0 : (int)n;
+        steps_bytes = ((size_t)(B + 1) * sizeof(long) + 15) / 16 * 16;
+        segments = (size_t)teams * row_groups * 2 * Shape::ROWS;
+    }
+    size_t bytes(int d) const { return teams == 0 ? 0 : steps_bytes + segments * (d + 2) * sizeof(float); }
 };
 
-template <typename Tag, int D, bool CODES, int RT>
-static int launch_cached(const CachedArgs& a, hipStream_t stream) {
-    constexpr int NW = 4, STG = D * (CODES ? 1 : 2) >= 256 ? 1 : 2;
-    using Shape = CachedShape<Tag, D, CODES, NW, STG, RT>;
-    auto kernel = fa_fwd_cache_kernel<Tag, D, CODES, NW, STG, RT>;
-    const double total = (double)a.B * a.c.H_kv * a.row_groups * a.splits;
-    if (total * NW * 64 >= 4294967296.0) return FA_ERR_LAUNCH;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(NW * 64), Shape::LDS, stream, a);
+template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT>
+static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t stream) {
+    const CachedDivision div(Shape{}, a.B, a.H, a.c.H_kv, a.T, max_len);
+    a.row_groups = div.row_groups;
+    a.teams = div.teams;
+    if (div.teams != 0) {
+        a.first_step = static_cast<long*>(workspace);
+        a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + div.steps_bytes);
+        a.state = a.part + div.segments * D;
+    }
+    const double total = (double)(div.teams != 0 ? div.teams : (double)a.B * a.c.H_kv) * a.row_groups;
+    if (total * 64 * kWaves >= 4294967296.0) return FA_ERR_LAUNCH;
+    constexpr int STG = Shape::WAVE_B / Shape::STAGE_B;
+    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, CODES, COLS, RT, kWaves, STG>), dim3((unsigned)total), dim3(kWaves * 64), Shape::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
-    if (a.splits > 1) {
+    if (div.teams != 0) {
         const long per = 256 / (D / 8), rows = (long)a.B * a.H * a.T;
-        hipLaunchKernelGGL((fa_join_kernel<Tag, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, a);
+        int ways = 1;  // the fewer rows there are, the more of them to a row
+        while (ways < per && ways < div.teams && rows * ways < 1024 * per) ways *= 2;
+        hipLaunchKernelGGL((fa_join_kernel<Tag, D, Shape::ROWS>), dim3((unsigned)((rows * ways + per - 1) / per)), dim3(256), 0, stream, a, ways);
         if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     }
     return FA_OK;
 }
 
-template <typename Tag, bool CODES>
-static int launch_cached_d(const CachedArgs& a, int d, int rt, hipStream_t stream) {
-    switch (d) {
-        case 64: return rt == 1 ? launch_cached<Tag, 64, CODES, 1>(a, stream) : launch_cached<Tag, 64, CODES, 2>(a, stream);
-        case 128: return rt == 1 ? launch_cached<Tag, 128, CODES, 1>(a, stream) : launch_cached<Tag, 128, CODES, 2>(a, stream);
-        default: return launch_cached<Tag, 256, CODES, 1>(a, stream);
-    }
-}
-
 }  // namespace
 
-size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int) {
-    const CachedDivision div(B, H, H_kv, T, d, max_len);
-    return div.splits == 1 ? 0 : (size_t)div.splits * B * H * T * (d + 2) * sizeof(float);
+size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype) {
+    return with_shape(H / H_kv * T, d, cache_dtype == FA_FP8_E4M3, [&](auto shape, auto...) { return CachedDivision(shape, B, H, H_kv, T, max_len).bytes(d); });
 }
 
 int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
                      void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream) {
-    const CachedDivision div(B, H, cache.H_kv, T, d, max_len);
-    float* part = static_cast<float*>(workspace);
-    float* state = div.splits == 1 ? nullptr : part + (size_t)div.splits * B * H * T * d;
-    const CachedArgs a = {q, o, cache, counts, tree, lse, part, state, B, H, T, tree_batches, div.row_groups, div.splits, div.chunk, scale};
-    const bool codes = cache.dtype == FA_FP8_E4M3;
-    if (dtype == FA_BF16) return codes ? launch_cached_d<bf16_tag, true>(a, d, div.rt, stream) : launch_cached_d<bf16_tag, false>(a, d, div.rt, stream);
-    return codes ? launch_cached_d<f16_tag, true>(a, d, div.rt, stream) : launch_cached_d<f16_tag, false>(a, d, div.rt, stream);
+    const CachedArgs a = {q, o, cache, counts, tree, lse, nullptr, nullptr, nullptr, B, H, T, tree_batches, 1, 0, scale};
+    return with_shape(H / cache.H_kv * T, d, cache.dtype == FA_FP8_E4M3, [&](auto shape, auto D, auto codes, auto cols, auto rt) {
+        using Shape = decltype(shape);
+        constexpr int d_ = decltype(D)::value, cols_ = decltype(cols)::value, rt_ = decltype(rt)::value;
+        constexpr bool codes_ = decltype(codes)::value;
+        return dtype == FA_BF16 ? launch_cached<bf16_tag, Shape, d_, codes_, cols_, rt_>(a, workspace, max_len, stream)
+                                : launch_cached<f16_tag, Shape, d_, codes_, cols_, rt_>(a, workspace, max_len, stream);
+    });
 }
 
 }  // namespace fa
