@@ -92,7 +92,9 @@ def lib():
         _lib = L
         if _native is not None:
             _native.bind(*(ctypes.cast(f, vp).value for f in (L.fa_fwd_gqa, L.fa_fwd_fp8_gqa, L.fa_fp8_quant_hadamard,
-                                                              L.fa_bwd_workspace_bytes, L.fa_bwd_gqa)))
+                                                              L.fa_bwd_workspace_bytes, L.fa_bwd_gqa, L.fa_rope, L.fa_rope_bwd,
+                                                              L.fa_cache_write, L.fa_cache_read, L.fa_fwd_cache_workspace_bytes,
+                                                              L.fa_fwd_cache)))
     return _lib
 
 
@@ -346,6 +348,10 @@ def fa_rope_frequencies(rot_dim, base=10000.0, scaling=FA_ROPE_PLAIN, factor=1.0
 
 
 def _rope(name, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out):
+    if _native is not None:
+        r = _native.rope(name == "fa_rope_bwd", q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, _stream)
+        if r is not None:
+            return _outputs(r, name)
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q and k must be [B,H,N,d] and [B,H_kv,N,d]")
     B, H, N, d = q.shape
@@ -413,6 +419,10 @@ def _check_cache(B, H_kv, d, k_pages, v_pages, block_table, lens, counts, k_scal
 def fa_cache_write(k, v, k_pages, v_pages, block_table, lens, counts=None, k_scales=None, v_scales=None):
     """k, v [B,H_kv,T,d] (contiguous rows) into the cache behind the lens[b] tokens that it holds: T of every sequence, or
     counts[b] of them.  Pages [n_pages,H_kv,page_size,d]: 16-bit, or e4m3 codes (uint8 or float8_e4m3fn) with scales."""
+    if _native is not None:
+        r = _native.cache_write(k, v, k_pages, v_pages, block_table, lens, counts, k_scales, v_scales, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_write")
     if k.dim() != 4:
         raise ValueError("k and v must be [B,H_kv,T,d]")
     B, H_kv, T, d = k.shape
@@ -431,6 +441,10 @@ def fa_cache_write(k, v, k_pages, v_pages, block_table, lens, counts=None, k_sca
 def fa_cache_read(k_pages, v_pages, block_table, lens, N=None, dtype=None, k_scales=None, v_scales=None, k=None, v=None):
     """The first min(lens[b], N) cached tokens of every sequence as k, v [B,H_kv,N,d]; the other rows stay as they are (in a tensor
     allocated here: uninitialised).  `dtype`: of allocated outputs (None: the cache's own 16-bit type, bfloat16 for codes)."""
+    if _native is not None:
+        r = _native.cache_read(k_pages, v_pages, block_table, lens, N, dtype, k_scales, v_scales, k, v, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_read")
     if k_pages.dim() != 4 or block_table.dim() != 2:
         raise ValueError("pages must be [n_pages,H_kv,page_size,d] and the block table [B,max_pages]")
     B, (_, H_kv, _, d) = block_table.shape[0], k_pages.shape
@@ -474,6 +488,11 @@ def fa_fwd_cache(q, k_pages, v_pages, block_table, lens, scale, tree=None, count
     """O, L of T new tokens of every sequence, q [B,H,T,d] (contiguous rows), over the cache, which holds them behind lens[b]
     others.  tree: int32 [B or 1, T, ceil(T / 32)] (fa_tree_words), None: a chain.  Rows from counts[b] on stay as they are (in
     tensors allocated here: uninitialised).  max_len: what lens[b] + T reaches at most, 0: the width of the block table."""
+    if _native is not None:
+        r = _native.fwd_cache(q, k_pages, v_pages, block_table, lens, scale, tree, counts, k_scales, v_scales, max_len, o, lse, workspace,
+                              _stream)
+        if r is not None:
+            return _outputs(r, "fa_fwd_cache")
     if q.dim() != 4 or k_pages.dim() != 4:
         raise ValueError("q must be [B,H,T,d] and pages [n_pages,H_kv,page_size,d]")
     B, H, T, d = q.shape

@@ -32,8 +32,10 @@ struct CachedArgs {
     Cache c;
     const int *counts, *tree;
     float* lse;
-    // the workspace: first steps of the sequences [B + 1], then for each workgroup two segments [rows][D] and [rows][2]
-    long* first_step;
+    // the workspace: where the segments of each sequence and head are [B H_kv], then for each workgroup two segments [rows][D] and [rows][2]
+    struct Segments {
+        int first, count;  // number of its first team's segment (2 team + 0 or 1); its teams.  The others' are their teams' first ones.
+    }* segments;
     float *part, *state;
     int B, H, T, tree_batches, row_groups, teams;  // teams 0: a workgroup to a sequence, head and row group
     float scale;
@@ -46,6 +48,7 @@ constexpr float kLazy = 8.0f;  // the reference of a row rises when a tile's max
 // What a sequence has: places before the new tokens, new tokens, all keys
 struct Extent {
     int len, count, keys;
+    Extent() = default;
     // (in scalar registers: the loads and divisions of one sequence's numbers come out in vector ones)
     __device__ __forceinline__ void make_uniform() {
         len = __builtin_amdgcn_readfirstlane(len);
@@ -69,27 +72,16 @@ static __device__ __forceinline__ long readlane64(long v, int lane) {
     return (long)((uint64_t)lo | (uint64_t)hi << 32);
 }
 
-// Calls f(b, steps before sequence b, of all heads) by lane over all sequences, 64 at a time, until it returns true; returns the
-// steps of all sequences that were looked at.
-template <int STEP, typename F>
-static __device__ __forceinline__ long scan_steps(const CachedArgs& a, int lane, F&& f) {
-    long before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int b = b0 + lane;
-        long n = 0;
-        if (b < a.B) n = (long)Extent(a, b).steps<STEP>() * a.c.H_kv;
-        long upto = n;
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) {
-            const long y = __shfl_up(upto, x);
-            if (lane >= x) upto += y;
-        }
-        const bool done = f(b, before + upto - n, n);
-        before += readlane64(upto, 63);
-        if (done) break;
+// Teams 0 .. rest - 1 have share + 1 consecutive steps of all, the others share
+struct Shares {
+    long share, rest;
+    __device__ __forceinline__ Shares(long total, int teams) : share(total / teams), rest(total - share * teams) {}
+    __device__ __forceinline__ long first(long team) const { return team * share + min(team, rest); }
+    __device__ __forceinline__ long team_of(long step) const {
+        const long longer = rest * (share + 1);
+        return step < longer ? step / (share + 1) : rest + (step - longer) / share;
     }
-    return before;
-}
+};
 
 // x of this lane's row of 16 lanes and of the row next to it (rows 0 and 1, 2 and 3)
 static __device__ __forceinline__ HalfPair both_rows(float x) {
@@ -153,6 +145,17 @@ template <typename Tag, int D> struct Matrix<Tag, D, 16> {
     }
 };
 
+#ifndef X_NT
+#define X_NT " nt"
+#endif
+// global_to_lds_16B of what nobody else reads
+static __device__ __forceinline__ void once_to_lds_16B(const BufferWords& rsrc, uint32_t lds_base, int byte_off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen" X_NT " lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(byte_off), "s"(rsrc.w)
+                 : "memory", "m0");
+}
+
 // A wave's tiles of 32 keys in the LDS, as they are staged and read.  A tile is unpadded; 16-byte chunk c of row r sits at
 // c ^ swizzle(r), applied through the global address that a lane fetches, so that each 16 lanes of a row read (16 rows, one
 // chunk) and each 32 of a transposing read (8 rows, two chunks, or 4 and 4, or 16 and 1) hit every bank once, with rows of 64 to
@@ -193,7 +196,7 @@ struct CacheTile {
     __device__ __forceinline__ void request(const BufferWords (&rsrc)[2], uint32_t offset) const {
         static_for<NI>([&](auto n) __attribute__((always_inline)) {
             constexpr int i = decltype(n)::value, r = i * RPI;
-            global_to_lds_16B(rsrc[i / (NI / 2)], base + offset + i * 1024, (int)((src0 ^ (uint32_t)(swizzle(r) << 4)) + (r % 16) * ROWB));
+            once_to_lds_16B(rsrc[i / (NI / 2)], base + offset + i * 1024, (int)((src0 ^ (uint32_t)(swizzle(r) << 4)) + (r % 16) * ROWB));
         });
     }
     // the lane's 16 bytes k of its row in score tile kt
@@ -350,44 +353,62 @@ fa_fwd_cache_kernel(CachedArgs a) {
     const int wg = team, rg = __builtin_amdgcn_readfirstlane(team % a.row_groups);
     team = __builtin_amdgcn_readfirstlane(team / a.row_groups);
     const int H_kv = a.c.H_kv, group = a.H / H_kv, n_rows = group * a.T;
-    int b, kvh, step = 0, left;  // the first segment, and how many steps the team has
+    int b, kvh, step = 0, left = 0x7fffffff;  // the first segment, and how many steps the team has
+    Extent ext;
+    long pos = 0;
+    Shares shares(1, 1);
     if (a.teams == 0) {
         b = __builtin_amdgcn_readfirstlane(team / H_kv);
         kvh = __builtin_amdgcn_readfirstlane(team - b * H_kv);
-        left = 0x7fffffff;
+        ext = Extent(a, b);
+        ext.make_uniform();
     } else {
-        long* const first = wg == 0 && wave == 0 ? a.first_step : nullptr;
-        const long total = scan_steps<Shape::STEP>(a, lane, [&](int s, long before, long n) {
-            if (first && s < a.B) {
-                first[s] = before;
-                if (s == a.B - 1) first[a.B] = before + n;
+        // Lane i looks at sequences i, i + 64, ...: first for the sum of their steps, then for the one with the team's first
+        // step (again, if there are more than 64)
+        long total = 0, before = 0, n = 0, upto = 0;
+        Extent mine;
+        auto look_at = [&](int b0) __attribute__((always_inline)) {
+            n = 0;
+            if (b0 + lane < a.B) {
+                mine = Extent(a, b0 + lane);
+                n = (long)mine.steps<Shape::STEP>() * H_kv;
             }
-            return false;
-        });
-        const long share = (total + a.teams - 1) / a.teams, pos = team * share;
-        if (pos >= total) return;
-        left = __builtin_amdgcn_readfirstlane((int)min(share, total - pos));
-        int at_b = 0;
-        long at_first = 0;
-        scan_steps<Shape::STEP>(a, lane, [&](int s, long before, long n) {
-            const uint64_t here = __builtin_amdgcn_ballot_w64(pos < before + n);
-            if (here == 0) return false;
-            const int i = __builtin_ctzll(here);
-            at_b = __builtin_amdgcn_readlane(s, i);
-            at_first = readlane64(before, i);
-            return true;
-        });
-        b = __builtin_amdgcn_readfirstlane(at_b);
-        const int rel = (int)(pos - at_first), n = Extent(a, b).steps<Shape::STEP>();
-        kvh = __builtin_amdgcn_readfirstlane(rel / n);
-        step = __builtin_amdgcn_readfirstlane(rel - rel / n * n);
+            upto = n;
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) {
+                const long y = __shfl_up(upto, x);
+                if (lane >= x) upto += y;
+            }
+        };
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            look_at(b0);
+            total += readlane64(upto, 63);
+        }
+        shares = Shares(total, a.teams);
+        pos = shares.first(team);
+        left = __builtin_amdgcn_readfirstlane((int)(shares.first(team + 1) - pos));
+        if (left == 0) return;
+        int b0 = 0;
+        if (a.B > 64)
+            for (;; b0 += 64) {
+                look_at(b0);
+                const long here = readlane64(upto, 63);
+                if (pos < before + here) break;
+                before += here;
+            }
+        const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(pos < before + upto));  // (one there is)
+        b = b0 + i;
+        ext.len = __builtin_amdgcn_readlane(mine.len, i);
+        ext.count = __builtin_amdgcn_readlane(mine.count, i);
+        ext.keys = __builtin_amdgcn_readlane(mine.keys, i);
+        const int rel = (int)(pos - before - readlane64(upto - n, i)), steps = ext.steps<Shape::STEP>();
+        kvh = __builtin_amdgcn_readfirstlane(rel / steps);
+        step = __builtin_amdgcn_readfirstlane(rel - rel / steps * steps);
     }
 
     const Tile tile(lds_address(lds) + wave * Shape::WAVE_B, lane);
     const float sc = a.scale * kLog2e;
     for (int segment = 0;; segment = 1) {
-    Extent ext(a, b);
-    ext.make_uniform();
     const int n_steps = ext.steps<Shape::STEP>();
     const int now = min(n_steps - step, left);
     const bool whole = now == n_steps;
@@ -421,7 +442,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     };
     auto request_k = [&](int i, auto stage) __attribute__((always_inline)) {
         constexpr int st = decltype(stage)::value;
-        if ((i & 63) == 0) look_up(i);
+        if ((i & 63) == 0 && i > 0) look_up(i);
         rows[st][0] = UniformRow(row_lo, i & 63);
         rows[st][1] = UniformRow(row_hi, i & 63);
         BufferWords rsrc[2];
@@ -442,12 +463,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
         resources(a.c.v, i, rows[st], rsrc);
         tile.request(rsrc, st * Shape::STAGE_B + Tile::TILE_B);
     };
-    if (mine > 0)
-        static_for<STG>([&](auto st) {
-            request_k(st, st);
-            request_v(st, st);
-        });
-
     int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
     i32x4 qreg[RT][QS];
 #pragma unroll
@@ -461,6 +476,19 @@ fa_fwd_cache_kernel(CachedArgs a) {
             qreg[x][u] = *reinterpret_cast<const i32x4*>(q + at);
         }
     }
+    // Q is on its way while the table is read, and there before the first request: the compiler, which does not see the requests,
+    // would wait for Q inside the loop with a count that waits for them all
+    look_up(0);
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int u = 0; u < QS; ++u) asm volatile("" : "+v"(qreg[x][u]));
+    if (mine > 0)
+        static_for<STG>([&](auto st) {
+            request_k(st, st);
+            request_v(st, st);
+        });
+
     typename M::Acc acc[RT][NT];
     float m_run[RT], l_run[RT];
     float F = 0.f, inv_F = 0.f;  // codes: the power of two that P~ is divided by
@@ -708,80 +736,96 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 }
             }
         }
+    if (a.teams == 0) break;
+    if (step == 0 && rg == 0 && tid == 0)
+        a.segments[b * H_kv + kvh] = {2 * team + segment, whole ? 1 : (int)(shares.team_of(pos + n_steps - 1) - team) + 1};
     left -= now;
-    if (a.teams == 0 || left == 0) break;
+    if (left == 0) break;
+    pos += now;
     step = 0;
     if (++kvh == H_kv) {
         kvh = 0;
         ++b;
+        ext = Extent(a, b);
+        ext.make_uniform();
     }
     __syncthreads();  // the merge area is staged into again
     }
 }
 
-// Joins the segments of rows whose sequence several teams have.  D / 8 threads stand side by side on a row, 8 columns each, and
-// `ways` such groups (a power of two, at most 256 / (D / 8)) take its segments in turn and meet in the LDS.
+// Joins the segments of rows whose sequence several teams have.  A workgroup stands on 64 columns (8 to a thread) of 32 / ways
+// rows; `ways` (a power of two, at most 32) threads take a row's segments in turn, each with a reference of its own, and meet in
+// the LDS.
+constexpr int kJoinCols = 64;
 template <typename Tag, int D, int ROWS>
 __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
     using E = Elem<Tag>;
-    constexpr int TPR = D / 8, GROUPS = 256 / TPR;
-    __shared__ float meet[GROUPS][D + 4];
-    const int group = threadIdx.x / TPR, way = group & (ways - 1), c = (threadIdx.x % TPR) * 8;
-    const long n_rows = (long)a.B * a.H * a.T, row = ((long)blockIdx.x * GROUPS + group) / ways;
-    const int bh = (int)(min(row, n_rows - 1) / a.T), tok = (int)(row - (long)bh * a.T), b = bh / a.H, head = bh - b * a.H;
+    constexpr int TPR = kJoinCols / 8, GROUPS = 256 / TPR;
+    __shared__ float meet[GROUPS][kJoinCols + 4];  // and the reference and the sum
+    const int group = threadIdx.x / TPR, way = group & (ways - 1), c0 = (threadIdx.x % TPR) * 8, c = blockIdx.y * kJoinCols + c0;
+    const unsigned n_rows = (unsigned)a.B * a.H * a.T, row = blockIdx.x * (GROUPS / ways) + group / ways;
+    const unsigned bh = min(row, n_rows - 1) / a.T;
+    const int tok = row - bh * a.T, b = bh / (unsigned)a.H, head = bh - b * a.H;
     const int heads = a.H / a.c.H_kv, kvh = head / heads, in_group = (head - kvh * heads) * a.T + tok, rg = in_group / ROWS;
-    const long share = (a.first_step[a.B] + a.teams - 1) / a.teams, steps = (a.first_step[b + 1] - a.first_step[b]) / a.c.H_kv;
-    const long start = a.first_step[b] + kvh * steps, team0 = start / share;
-    const int n = (int)((start + steps - 1) / share - team0) + 1;
-    // of team team0 + s: the first segment of those that begin inside the sequence, the second of one that ends with its beginning
-    auto place = [&](int s) {
-        const long wg = (team0 + s) * a.row_groups + rg;
-        return (wg * 2 + (s == 0 && start != team0 * share)) * ROWS + (in_group - rg * ROWS);
-    };
-    const bool there = row < n_rows && n > 1 && tok < Extent(a, b).count;
-    float m_all = -INFINITY, l_all = 0.f;
+    const CachedArgs::Segments of = a.segments[b * a.c.H_kv + kvh];
+    const int count = a.counts ? a.counts[b] : a.T;
+    const bool there = row < n_rows && of.count > 1 && tok < count;
+    float m = -INFINITY, l = 0.f;
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (there) {
-        // the reference: each of the group's threads looks at some of the segments
-        for (int s = threadIdx.x % TPR; s < n; s += TPR) m_all = fmaxf(m_all, a.state[2 * place(s)]);
-#pragma unroll
-        for (int x = 1; x < TPR; x <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, x));
-        const float m_ref = m_all == -INFINITY ? 0.f : m_all;
+    if (there)
 #pragma unroll 4
-        for (int s = way; s < n; s += ways) {
-            const long at = place(s);
-            const float f = fast_exp2(a.state[2 * at] - m_ref);
-            l_all += f * a.state[2 * at + 1];
+        for (int s = way; s < of.count; s += ways) {
+            const long segment = s == 0 ? of.first : (of.first & ~1) + 2 * s;
+            const long at = (((segment >> 1) * a.row_groups + rg) * 2 + (segment & 1)) * ROWS + (in_group - rg * ROWS);
+            const float sm = a.state[2 * at], sl = a.state[2 * at + 1];
             const f32x4 lo = *reinterpret_cast<const f32x4*>(a.part + at * D + c), hi = *reinterpret_cast<const f32x4*>(a.part + at * D + c + 4);
+            const float top = fmaxf(m, sm), ref = top == -INFINITY ? 0.f : top, f = fast_exp2(m - ref), g = fast_exp2(sm - ref);
+            m = top;
+            l = l * f + sl * g;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                y[e] = __builtin_fmaf(f, lo[e], y[e]);
-                y[4 + e] = __builtin_fmaf(f, hi[e], y[4 + e]);
+                y[e] = y[e] * f + lo[e] * g;
+                y[4 + e] = y[4 + e] * f + hi[e] * g;
             }
         }
-    }
     if (ways > 1) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) meet[group][c + e] = y[e];
-        if (c == 0) meet[group][D] = l_all;
+        for (int e = 0; e < 8; ++e) meet[group][c0 + e] = y[e];
+        if (c0 == 0) {
+            meet[group][kJoinCols] = m;
+            meet[group][kJoinCols + 1] = l;
+        }
         __syncthreads();
-        if (way == 0)
-            for (int w = 1; w < ways; ++w) {
+        if (way == 0) {
+            const int used = min(ways, of.count);
+            float top = m;
+            for (int w = 1; w < used; ++w) top = fmaxf(top, meet[group + w][kJoinCols]);
+            const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(m - ref);
+            l *= f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] += meet[group + w][c + e];
-                l_all += meet[group + w][D];
+            for (int e = 0; e < 8; ++e) y[e] *= f;
+            for (int w = 1; w < used; ++w) {
+                const float g = fast_exp2(meet[group + w][kJoinCols] - ref);
+                l += meet[group + w][kJoinCols + 1] * g;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] += meet[group + w][c0 + e] * g;
             }
+            m = top;
+        }
     }
     if (!there || way != 0) return;
-    const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
     i32x4 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = E::pack2(y[2 * e] * inv, y[2 * e + 1] * inv);
     uint16_t* o = static_cast<uint16_t*>(const_cast<void*>(a.o.p)) + (b * a.o.batch + head * a.o.head + tok * a.o.token);
     *reinterpret_cast<i32x4*>(o + c) = w;
-    if (c == 0) a.lse[row] = (m_all + log2f(l_all)) * kLn2;
+    if (c == 0) a.lse[row] = (m + log2f(l)) * kLn2;
 }
 
+#ifndef X_JOIN
+#define X_JOIN 256
+#endif
 #ifndef X_OVER
 #define X_OVER 1
 #endif
@@ -815,7 +859,7 @@ static auto with_shape(int rows, int d, bool codes, F&& f) {
 // How a call is divided.  (The shapes do not depend on the 16-bit type.)
 struct CachedDivision {
     int row_groups, teams;
-    size_t steps_bytes, segments;  // of the workspace: the sequences' first steps; segments' rows
+    size_t table_bytes, rows;  // of the workspace: where segments are; the segments' rows
     template <typename Shape>
     CachedDivision(const Shape&, int B, int H, int H_kv, int T, int max_len) {
         row_groups = (H / H_kv * T + Shape::ROWS - 1) / Shape::ROWS;
@@ -823,10 +867,10 @@ struct CachedDivision {
         long n = slots / row_groups > 1 ? slots / row_groups : 1;
         if ((double)items * most < n) n = items * most;
         teams = most <= 4 || items * row_groups >= 4 * slots ? 0 : (int)n;
-        steps_bytes = ((size_t)(B + 1) * sizeof(long) + 15) / 16 * 16;
-        segments = (size_t)teams * row_groups * 2 * Shape::ROWS;
+        table_bytes = ((size_t)items * sizeof(CachedArgs::Segments) + 15) / 16 * 16;
+        rows = (size_t)teams * row_groups * 2 * Shape::ROWS;
     }
-    size_t bytes(int d) const { return teams == 0 ? 0 : steps_bytes + segments * (d + 2) * sizeof(float); }
+    size_t bytes(int d) const { return teams == 0 ? 0 : table_bytes + rows * (d + 2) * sizeof(float); }
 };
 
 template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT>
@@ -835,9 +879,9 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
     a.row_groups = div.row_groups;
     a.teams = div.teams;
     if (div.teams != 0) {
-        a.first_step = static_cast<long*>(workspace);
-        a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + div.steps_bytes);
-        a.state = a.part + div.segments * D;
+        a.segments = static_cast<CachedArgs::Segments*>(workspace);
+        a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + div.table_bytes);
+        a.state = a.part + div.rows * D;
     }
     const double total = (double)(div.teams != 0 ? div.teams : (double)a.B * a.c.H_kv) * a.row_groups;
     if (total * 64 * kWaves >= 4294967296.0) return FA_ERR_LAUNCH;
@@ -845,10 +889,10 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
     hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, CODES, COLS, RT, kWaves, STG>), dim3((unsigned)total), dim3(kWaves * 64), Shape::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     if (div.teams != 0) {
-        const long per = 256 / (D / 8), rows = (long)a.B * a.H * a.T;
-        int ways = 1;  // the fewer rows there are, the more of them to a row
-        while (ways < per && ways < div.teams && rows * ways < 1024 * per) ways *= 2;
-        hipLaunchKernelGGL((fa_join_kernel<Tag, D, Shape::ROWS>), dim3((unsigned)((rows * ways + per - 1) / per)), dim3(256), 0, stream, a, ways);
+        const long rows = (long)a.B * a.H * a.T;
+        int ways = 1;  // the fewer rows there are, the more threads to a row
+        while (ways < 32 && ways < div.teams && rows * ways < 32 * X_JOIN) ways *= 2;
+        hipLaunchKernelGGL((fa_join_kernel<Tag, D, Shape::ROWS>), dim3((unsigned)((rows * ways + 31) / 32), D / kJoinCols), dim3(256), 0, stream, a, ways);
         if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     }
     return FA_OK;
