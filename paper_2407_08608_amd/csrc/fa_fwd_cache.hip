@@ -67,21 +67,26 @@ struct Extent {
     }
 };
 
-static __device__ __forceinline__ long readlane64(long v, int lane) {
-    const uint32_t lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
-    return (long)((uint64_t)lo | (uint64_t)hi << 32);
-}
-
-// Teams 0 .. rest - 1 have share + 1 consecutive steps of all, the others share
+// `of` things in order to `among`: the first of % among of them have one more.  (Steps of all sequences are fewer than 2^31.)
 struct Shares {
-    long share, rest;
-    __device__ __forceinline__ Shares(long total, int teams) : share(total / teams), rest(total - share * teams) {}
-    __device__ __forceinline__ long first(long team) const { return team * share + min(team, rest); }
-    __device__ __forceinline__ long team_of(long step) const {
-        const long longer = rest * (share + 1);
-        return step < longer ? step / (share + 1) : rest + (step - longer) / share;
+    uint32_t each, rest;
+    __device__ __forceinline__ Shares(uint32_t of, uint32_t among) : each(of / among), rest(of - each * among) {}
+    __device__ __forceinline__ uint32_t first(uint32_t i) const { return i * each + min(i, rest); }
+    __device__ __forceinline__ uint32_t owner(uint32_t thing) const {
+        const uint32_t longer = rest * (each + 1);
+        return thing < longer ? thing / (each + 1) : rest + (thing - longer) / each;
     }
 };
+
+// x summed up to and with this lane
+static __device__ __forceinline__ uint32_t sum_upto(uint32_t x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
 
 // x of this lane's row of 16 lanes and of the row next to it (rows 0 and 1, 2 and 3)
 static __device__ __forceinline__ HalfPair both_rows(float x) {
@@ -326,7 +331,7 @@ struct CachedShape {
     static constexpr int STEP = 32 * NW;                   // keys of a step
     static constexpr int SCALE_B = CODES ? 256 : 0;        // of a tile: 32 scales of K, 32 of V
     static constexpr int STAGE_B = 2 * Tile::TILE_B + SCALE_B, WAVE_B = STG * STAGE_B;
-    static constexpr int MERGE_COLS = COLS == 16 && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
+    static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
     static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * ROWS * 3 * 4;
     static constexpr int LDS = (NW * WAVE_B > MERGE_B ? NW * WAVE_B : MERGE_B) + STATE_B;
     static constexpr int WAVES = COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;  // to a SIMD, by registers
@@ -343,6 +348,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     using PE = Elem<typename Tile::PE>;
     using E = Elem<Tag>;
     constexpr int NS = M::NS, NT = M::NT, NI = Tile::NI, X = CODES ? 1 : 0, ACC = sizeof(typename M::Acc) / 4;
+    constexpr bool ACCUMULATION = Shape::WAVES == 1;  // more than 256 registers: accumulators in the half for matrix results
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -355,8 +361,9 @@ fa_fwd_cache_kernel(CachedArgs a) {
     const int H_kv = a.c.H_kv, group = a.H / H_kv, n_rows = group * a.T;
     int b, kvh, step = 0, left = 0x7fffffff;  // the first segment, and how many steps the team has
     Extent ext;
-    long pos = 0;
+    uint32_t pos = 0;  // of the team's first step among all
     Shares shares(1, 1);
+    int own_parts = 0;  // how many teams have the sequence and head, where each team has one
     if (a.teams == 0) {
         b = __builtin_amdgcn_readfirstlane(team / H_kv);
         kvh = __builtin_amdgcn_readfirstlane(team - b * H_kv);
@@ -365,45 +372,62 @@ fa_fwd_cache_kernel(CachedArgs a) {
     } else {
         // Lane i looks at sequences i, i + 64, ...: first for the sum of their steps, then for the one with the team's first
         // step (again, if there are more than 64)
-        long total = 0, before = 0, n = 0, upto = 0;
+        uint32_t total = 0, before = 0, n = 0, upto = 0;
         Extent mine;
         auto look_at = [&](int b0) __attribute__((always_inline)) {
             n = 0;
             if (b0 + lane < a.B) {
                 mine = Extent(a, b0 + lane);
-                n = (long)mine.steps<Shape::STEP>() * H_kv;
+                n = (uint32_t)mine.steps<Shape::STEP>();
             }
-            upto = n;
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) {
-                const long y = __shfl_up(upto, x);
-                if (lane >= x) upto += y;
-            }
+            upto = sum_upto(n, lane);
         };
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             look_at(b0);
-            total += readlane64(upto, 63);
+            total += __builtin_amdgcn_readlane(upto, 63);
         }
-        shares = Shares(total, a.teams);
-        pos = shares.first(team);
-        left = __builtin_amdgcn_readfirstlane((int)(shares.first(team + 1) - pos));
-        if (left == 0) return;
-        int b0 = 0;
-        if (a.B > 64)
-            for (;; b0 += 64) {
-                look_at(b0);
-                const long here = readlane64(upto, 63);
-                if (pos < before + here) break;
-                before += here;
-            }
-        const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(pos < before + upto));  // (one there is)
-        b = b0 + i;
+        shares = Shares(total * H_kv, a.teams);
+        // Where a share of at most one step more lets each team stay with one sequence and head, it does: no second start
+        uint32_t parts = 0, parts_upto = 0;
+        if (a.B <= 64) {
+            parts = (n + shares.each) / (shares.each + 1);
+            parts_upto = sum_upto(parts, lane);
+        }
+        const uint32_t used = __builtin_amdgcn_readlane(parts_upto, 63) * H_kv;
+        int i;
+        if (a.B <= 64 && used <= (uint32_t)a.teams) {
+            if ((uint32_t)team >= used) return;
+            i = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)team < parts_upto * H_kv));
+            b = i;
+            const uint32_t k = __builtin_amdgcn_readlane(parts, i), rel = team - (__builtin_amdgcn_readlane(parts_upto, i) - k) * H_kv;
+            kvh = __builtin_amdgcn_readfirstlane((int)(rel / k));
+            const uint32_t part = __builtin_amdgcn_readfirstlane((int)(rel - rel / k * k));
+            const Shares inside(__builtin_amdgcn_readlane(n, i), k);
+            step = __builtin_amdgcn_readfirstlane((int)inside.first(part));
+            left = __builtin_amdgcn_readfirstlane((int)inside.first(part + 1)) - step;
+            own_parts = (int)k;
+        } else {
+            pos = __builtin_amdgcn_readfirstlane(shares.first(team));
+            left = __builtin_amdgcn_readfirstlane((int)(shares.first(team + 1) - pos));
+            if (left == 0) return;
+            int b0 = 0;
+            if (a.B > 64)
+                for (;; b0 += 64) {
+                    look_at(b0);
+                    const uint32_t here = __builtin_amdgcn_readlane(upto, 63) * H_kv;
+                    if (pos < before + here) break;
+                    before += here;
+                }
+            i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(pos < before + upto * H_kv));  // (one there is)
+            b = b0 + i;
+            const uint32_t steps = __builtin_amdgcn_readlane(n, i);
+            const uint32_t rel = pos - before - (__builtin_amdgcn_readlane(upto, i) - steps) * H_kv;
+            kvh = __builtin_amdgcn_readfirstlane((int)(rel / steps));
+            step = __builtin_amdgcn_readfirstlane((int)(rel - rel / steps * steps));
+        }
         ext.len = __builtin_amdgcn_readlane(mine.len, i);
         ext.count = __builtin_amdgcn_readlane(mine.count, i);
         ext.keys = __builtin_amdgcn_readlane(mine.keys, i);
-        const int rel = (int)(pos - before - readlane64(upto - n, i)), steps = ext.steps<Shape::STEP>();
-        kvh = __builtin_amdgcn_readfirstlane(rel / steps);
-        step = __builtin_amdgcn_readfirstlane(rel - rel / steps * steps);
     }
 
     const Tile tile(lds_address(lds) + wave * Shape::WAVE_B, lane);
@@ -419,14 +443,15 @@ fa_fwd_cache_kernel(CachedArgs a) {
     long row_lo = -1, row_hi = -1;
     auto look_up = [&](int first) __attribute__((always_inline)) {
         const int key = key0 + 32 * (wave + NW * (first + lane));
-        auto of = [&](int k) -> long {
-            if (k >= key1 || k < key0) return -1;
-            const int entry = k / a.c.page_size, page = a.c.block_table[(long)b * a.c.max_pages + entry];
-            if (page < 0 || page >= a.c.n_pages) return -1;
-            return ((long)page * H_kv + kvh) * a.c.page_size + (k - entry * a.c.page_size);
-        };
-        row_lo = of(key);
-        row_hi = of(key + 16);
+        // (both lookups at once, whether or not the second page is the first)
+        const int page_size = a.c.page_size, entry = (unsigned)max(key, 0) / (unsigned)page_size, slot = key - entry * page_size;
+        const bool next = slot + 16 >= page_size;
+        const int entry_hi = entry + next, slot_hi = slot + 16 - (next ? page_size : 0);
+        const int* const table = a.c.block_table + (long)b * a.c.max_pages;
+        const bool in_lo = key >= key0 && key < key1, in_hi = key >= key0 && key < key1 - 16;
+        const int page = in_lo ? table[entry] : -1, page_hi = in_hi ? table[entry_hi] : -1;
+        row_lo = page < 0 || page >= a.c.n_pages ? -1 : ((long)page * H_kv + kvh) * page_size + slot;
+        row_hi = page_hi < 0 || page_hi >= a.c.n_pages ? -1 : ((long)page_hi * H_kv + kvh) * page_size + slot_hi;
     };
     // requests K of the wave's tile i into stage st, and its V when that stage's V has been read
     UniformRow rows[STG][2];
@@ -602,7 +627,11 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                     for (int x = 0; x < RT; ++x)
 #pragma unroll
-                        for (int dt = 0; dt < NT; ++dt) acc[x][dt] *= down;
+                        for (int dt = 0; dt < NT; ++dt) {
+                            if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));
+                            acc[x][dt] *= down;
+                            if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));
+                        }
                 }
 #pragma unroll
                 for (int r = 0; r < NS; ++r) vscale[r] *= inv_F;
@@ -620,7 +649,11 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     m_run[x] = raise ? m_new : m_run[x];
                     l_run[x] *= corr;
 #pragma unroll
-                    for (int dt = 0; dt < NT; ++dt) acc[x][dt] *= corr;
+                    for (int dt = 0; dt < NT; ++dt) {
+                        if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));  // (copied out here, not in every tile)
+                        acc[x][dt] *= corr;
+                        if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));
+                    }
                 }
                 const float mb = m_run[x] == -INFINITY ? 0.f : m_run[x] * sc;  // a row that has seen nothing yet: P = 0
                 float ps[4];
@@ -738,7 +771,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
         }
     if (a.teams == 0) break;
     if (step == 0 && rg == 0 && tid == 0)
-        a.segments[b * H_kv + kvh] = {2 * team + segment, whole ? 1 : (int)(shares.team_of(pos + n_steps - 1) - team) + 1};
+        a.segments[b * H_kv + kvh] = {2 * team + segment, own_parts ? own_parts : whole ? 1 : (int)shares.owner(pos + n_steps - 1) - team + 1};
     left -= now;
     if (left == 0) break;
     pos += now;
@@ -875,7 +908,9 @@ struct CachedDivision {
 
 template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT>
 static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t stream) {
-    const CachedDivision div(Shape{}, a.B, a.H, a.c.H_kv, a.T, max_len);
+    CachedDivision div(Shape{}, a.B, a.H, a.c.H_kv, a.T, max_len);
+    // (steps are counted in 32 bits, and there may be as many as there are places, whatever was expected)
+    if ((double)a.B * a.c.H_kv * ((double)a.c.max_pages * a.c.page_size / Shape::STEP + 1) >= 2147483647.0) div.teams = 0;
     a.row_groups = div.row_groups;
     a.teams = div.teams;
     if (div.teams != 0) {
