@@ -25,9 +25,13 @@ struct RopeArgs {
 template <int DTYPE> struct RowChunk {  // 8 elements as floats
     static constexpr int ELEM = DTYPE == FA_F32 ? 4 : 2;
     i32x4 w[ELEM / 2];
+    template <bool ONCE>
     __device__ __forceinline__ void load(const char* p) {
 #pragma unroll
-        for (int i = 0; i < ELEM / 2; ++i) w[i] = *reinterpret_cast<const i32x4*>(p + 16 * i);
+        for (int i = 0; i < ELEM / 2; ++i) {
+            const i32x4* at = reinterpret_cast<const i32x4*>(p + 16 * i);
+            w[i] = ONCE ? __builtin_nontemporal_load(at) : *at;
+        }
     }
     __device__ __forceinline__ void store(char* p) const {
 #pragma unroll
@@ -57,7 +61,7 @@ template <int DTYPE> struct RowChunk {  // 8 elements as floats
     }
 };
 
-template <int D, int DTYPE, bool INTERLEAVED>
+template <int D, int DTYPE, bool INTERLEAVED, bool ONCE>
 __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
     constexpr int TPR = D / 16, ELEM = RowChunk<DTYPE>::ELEM;  // threads per token
     const unsigned token = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
@@ -90,8 +94,8 @@ __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
         char* y = static_cast<char*>(const_cast<void*>(yr.p)) + (b * yr.batch + head * yr.head + n * yr.token) * ELEM;
         if (!turned && x == y) continue;
         RowChunk<DTYPE> w0, w1;
-        w0.load(x + c0 * 8 * ELEM);
-        w1.load(x + c1 * 8 * ELEM);
+        w0.template load<ONCE>(x + c0 * 8 * ELEM);
+        w1.template load<ONCE>(x + c1 * 8 * ELEM);
         if (turned) {
             float f0[8], f1[8];
             w0.get(f0);
@@ -121,10 +125,18 @@ __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
     }
 }
 
+// Whether the inputs are read past the caches: so many bytes do not stay there until they are read anyway, and push the outputs out,
+// which the next call reads.  us, kept / past, MiB of input; after other inputs | after a launch that writes them (included):
+//   8 5.9 / 5.9 | 13.5 / 13.6;  32 12.2 / 13.7 | 26.6 / 26.3;  64 24.7 / 24.9 | 41.5 / 39.8;  80 33.5 / 30.0 | 48.2 / 46.7;
+//   109 46.9 / 39.0 | 61.0 / 59.6;  128 55.1 / 44.8 | 68.7 / 73.3;  188 78.0 / 78.8 | 106 / 96.5;  256 99.9 / 99.9 | 161 / 133
+constexpr double kReadOnce = 72.0 * 1024 * 1024;
+
 template <int D, int DTYPE>
 static int launch_rope_d(const RopeArgs& a, int interleaved, const dim3& grid, hipStream_t stream) {
-    if (interleaved) hipLaunchKernelGGL((fa_rope_kernel<D, DTYPE, true>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((fa_rope_kernel<D, DTYPE, false>), grid, dim3(256), 0, stream, a);
+    const bool once = (double)a.B * a.heads * a.N * D * RowChunk<DTYPE>::ELEM > kReadOnce;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+    if (interleaved) once ? go(fa_rope_kernel<D, DTYPE, true, true>) : go(fa_rope_kernel<D, DTYPE, true, false>);
+    else once ? go(fa_rope_kernel<D, DTYPE, false, true>) : go(fa_rope_kernel<D, DTYPE, false, false>);
     return hipGetLastError() == hipSuccess ? FA_OK : FA_ERR_LAUNCH;
 }
 
