@@ -24,6 +24,18 @@
 //     instructions for a tile.
 #include "fa_device.h"
 #include "fa_launch.h"
+#ifndef X_ROWS
+#define X_ROWS 64
+#endif
+#ifndef X_S64
+#define X_S64 3
+#endif
+#ifndef X_S128
+#define X_S128 2
+#endif
+#ifndef X_SHLOAD
+#define X_SHLOAD global_to_lds_16B
+#endif
 
 namespace fa {
 
@@ -204,6 +216,13 @@ struct CacheTile {
             once_to_lds_16B(rsrc[i / (NI / 2)], base + offset + i * 1024, (int)((src0 ^ (uint32_t)(swizzle(r) << 4)) + (r % 16) * ROWB));
         });
     }
+    // those of 16 rows; `src`: src0, with the swizzle of the second 16 rows where it is these
+    __device__ __forceinline__ void request_half(const BufferWords& rsrc, uint32_t offset, uint32_t src) const {
+        static_for<NI / 2>([&](auto n) __attribute__((always_inline)) {
+            constexpr int i = decltype(n)::value, r = i * RPI;
+            X_SHLOAD(rsrc, base + offset + i * 1024, (int)((src ^ (uint32_t)(swizzle(r) << 4)) + r * ROWB));
+        });
+    }
     // the lane's 16 bytes k of its row in score tile kt
     template <int K, int KT>
     __device__ __forceinline__ i32x4 row_read(uint32_t offset) const {
@@ -225,10 +244,9 @@ struct CacheTile {
     }
 
     // An infinity or a NaN in V of a new token is no business of the rows that do not see it, and a product with P = 0 would
-    // make it theirs.  So where a tile has one (not_finite), matrix products of ones count for each row and column what it sees
-    // of them (add_not_finite), and it is a zero for the product with P (clear_not_finite).
+    // make it theirs.  So where a tile has one (not_finite) it is a zero for the product (clear_not_finite), and the rows that see it
+    // get it at the end.
     static constexpr int EXPONENT = CODES ? 0x7F7F7F7F : std::is_same_v<Tag, bf16_tag> ? 0x7F807F80 : 0x7C007C00;
-    static constexpr int ONE = std::is_same_v<PE, bf16_tag> ? 0x3F803F80 : 0x3C003C00;  // two ones
     // the elements of a word that are not finite, all bits of each
     static __device__ __forceinline__ uint32_t odd_ones(uint32_t w) {
         const uint32_t x = (w & EXPONENT) ^ EXPONENT;  // 0 where the exponent (of a code: all but the sign) is full
@@ -239,12 +257,6 @@ struct CacheTile {
             const uint32_t full = (0x80008000u - x) & 0x80008000u;
             return (full >> 15) * 0xFFFFu;
         }
-    }
-    // of a word of 16-bit elements: ones where an element is an infinity of this sign, or a NaN
-    static __device__ __forceinline__ uint32_t infinite(uint32_t w, bool negative) {
-        const uint32_t sign = ((w & 0x80008000u) >> 15) * 0xFFFFu;
-        const uint32_t nan = ((((w & ~(EXPONENT | 0x80008000u)) + 0x7FFF7FFFu) & 0x80008000u) >> 15) * 0xFFFFu;
-        return odd_ones(w) & ((negative ? sign : ~sign) | nan) & ONE;
     }
     __device__ __forceinline__ bool not_finite(uint32_t offset, int lane) const {
         uint32_t any = 0;
@@ -267,36 +279,6 @@ struct CacheTile {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    // `seen`: bit(r) is what the lane's row sees of its part's keys
-    __device__ __forceinline__ void add_not_finite(uint32_t offset, uint32_t seen, typename M::Acc (&acc)[M::NT]) const {
-        i32x4 ones[M::SLABS];
-#pragma unroll
-        for (int r = 0; r < M::NS; r += 2) {
-            const uint32_t two = seen >> M::bit(r);
-            ones[r >> 3][(r >> 1) & 3] = (int)((two & 1 ? 0xFFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u)) & ONE;
-        }
-        static_for<M::NT>([&](auto d) __attribute__((always_inline)) {
-            constexpr int dt = decltype(d)::value;
-#pragma unroll
-            for (int negative = 0; negative < (CODES ? 1 : 2); ++negative) {
-                typename M::Acc count = {};
-                static_for<M::SLABS>([&](auto sl) __attribute__((always_inline)) {
-                    constexpr int slab = decltype(sl)::value;
-                    i32x4 w = columns<dt, slab>(offset);
-                    if constexpr (CODES) {
-                        w = from_codes<f16_tag>((int)odd_ones(w[0]) & 0x38383838, (int)odd_ones(w[1]) & 0x38383838);  // 0x38: 1
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = (int)infinite(w[e], negative);
-                    }
-                    count = PM::mma(w, ones[slab], count);
-                });
-                const float what = CODES ? __builtin_nanf("") : negative ? -INFINITY : INFINITY;  // a NaN counts as both
-#pragma unroll
-                for (int r = 0; r < (int)(sizeof(count) / 4); ++r) acc[dt][r] += count[r] > 0.f ? what : 0.f;
-            }
-        });
-    }
 };
 
 // Asynchronous copy of 4 bytes per lane from an address per lane to lds_base + 4 lane
@@ -306,6 +288,9 @@ static __device__ __forceinline__ void global_to_lds_4B(const float* p, uint32_t
                  : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(p)
                  : "memory", "m0");
 }
+
+// The waves of a workgroup meet; what they have asked of the LDS is done
+static __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <int N>
 static __device__ __forceinline__ void wait_vmcnt() {
@@ -324,24 +309,31 @@ struct UniformRow {
     __device__ __forceinline__ long index() const { return (long)((uint64_t)(uint32_t)(lo & ~none()) | (uint64_t)(uint32_t)(hi & ~none()) << 32); }
 };
 
-template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG>
+// FORM: the waves of a workgroup either share its rows and divide the keys (kDivideKeys), or they have RT tiles of rows each and
+// share the keys, which they stage together (kShareKeys).
+enum Form { kDivideKeys, kShareKeys };
+template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG, int FORM>
 struct CachedShape {
     using Tile = CacheTile<Tag, D, CODES, COLS>;
-    static constexpr int ROWS = COLS * RT;                 // of a workgroup
-    static constexpr int STEP = 32 * NW;                   // keys of a step
-    static constexpr int SCALE_B = CODES ? 256 : 0;        // of a tile: 32 scales of K, 32 of V
-    static constexpr int STAGE_B = 2 * Tile::TILE_B + SCALE_B, WAVE_B = STG * STAGE_B;
+    static constexpr bool SHARED = FORM == kShareKeys;
+    static constexpr int ROWS = COLS * RT * (SHARED ? NW : 1);  // of a workgroup
+    static constexpr int STEP = 32 * NW;                        // keys of a step
+    static constexpr int SCALE_B = CODES ? 256 : 0;             // of a tile: 32 scales of K, 32 of V
+    static constexpr int STAGE_B = 2 * Tile::TILE_B + SCALE_B, STAGES_B = STG * STAGE_B * (SHARED ? 1 : NW);
     static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
-    static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * ROWS * 3 * 4;
-    static constexpr int LDS = (NW * WAVE_B > MERGE_B ? NW * WAVE_B : MERGE_B) + STATE_B;
-    static constexpr int WAVES = COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;  // to a SIMD, by registers
-    static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;  // workgroups of four waves
+    static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 3 * 4 + NW * 4;
+    static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
+    // workgroups (of four waves) to a CU, by registers
+    static constexpr int WAVES = SHARED ? (D == 64 ? X_S64 : D == 128 ? X_S128 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
+    static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;
 };
 
-template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG>
-__global__ void __launch_bounds__(NW * 64, (CachedShape<Tag, D, CODES, COLS, RT, NW, STG>::WAVES))
+template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG, int FORM>
+__global__ void __launch_bounds__(NW * 64, (CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>::WAVES))
 fa_fwd_cache_kernel(CachedArgs a) {
-    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG>;
+    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>;
+    constexpr bool SHARED = Shape::SHARED;
+    constexpr int KW = SHARED ? 1 : NW, RW = SHARED ? NW : 1;  // waves that divide keys, that have rows of their own
     using Tile = typename Shape::Tile;
     using M = typename Tile::M;
     using PM = typename Tile::PM;
@@ -352,7 +344,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int col = lane % COLS, part = lane / COLS;
+    const int col = lane % COLS, part = lane / COLS, kw = SHARED ? 0 : wave, rw = SHARED ? wave : 0;
 
     // which rows and keys: a team's workgroups side by side on one XCD
     int team = xcd_run(blockIdx.x, gridDim.x);
@@ -430,19 +422,19 @@ fa_fwd_cache_kernel(CachedArgs a) {
         ext.keys = __builtin_amdgcn_readlane(mine.keys, i);
     }
 
-    const Tile tile(lds_address(lds) + wave * Shape::WAVE_B, lane);
+    const Tile tile(lds_address(lds) + kw * (STG * Shape::STAGE_B), lane);
     const float sc = a.scale * kLog2e;
     for (int segment = 0;; segment = 1) {
     const int n_steps = ext.steps<Shape::STEP>();
     const int now = min(n_steps - step, left);
     const bool whole = now == n_steps;
     const int key0 = step * Shape::STEP, key1 = step + now == n_steps ? ext.keys : key0 + now * Shape::STEP;
-    const int n_tiles = (int)(((unsigned)max(key1 - key0, 0) + 31) / 32), mine = n_tiles > wave ? (n_tiles - wave + NW - 1) / NW : 0;
+    const int n_tiles = (int)(((unsigned)max(key1 - key0, 0) + 31) / 32), mine = n_tiles > kw ? (n_tiles - kw + KW - 1) / KW : 0;
 
     // rows (of all pages' rows, heads included) of the wave's tiles: lane i has tile i of 64, two times 16 places; -1: no page
     long row_lo = -1, row_hi = -1;
     auto look_up = [&](int first) __attribute__((always_inline)) {
-        const int key = key0 + 32 * (wave + NW * (first + lane));
+        const int key = key0 + 32 * (kw + KW * (first + lane));
         // (both lookups at once, whether or not the second page is the first)
         const int page_size = a.c.page_size, entry = (unsigned)max(key, 0) / (unsigned)page_size, slot = key - entry * page_size;
         const bool next = slot + 16 >= page_size;
@@ -456,7 +448,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // requests K of the wave's tile i into stage st, and its V when that stage's V has been read
     UniformRow rows[STG][2];
     auto resources = [&](const void* pages, int i, const UniformRow (&row)[2], BufferWords (&rsrc)[2]) __attribute__((always_inline)) {
-        const int there = key1 - (key0 + 32 * (wave + NW * i));
+        const int there = key1 - (key0 + 32 * (kw + KW * i));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             int n = max(there - 16 * h, 0);
@@ -477,7 +469,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
             long row = rows[st][0].index(), upper = rows[st][1].index();
             asm volatile("" : "+v"(row), "+v"(upper));  // (a choice between vector registers, not between places in memory)
             row = lane & 16 ? upper : row;
-            const int there = key1 - (key0 + 32 * (wave + NW * i));
+            const int there = key1 - (key0 + 32 * (kw + KW * i));
             const long at = (lane & 31) >= there ? 0 : row + (lane & 15);
             global_to_lds_4B((lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + st * Shape::STAGE_B + 2 * Tile::TILE_B);
         }
@@ -488,11 +480,34 @@ fa_fwd_cache_kernel(CachedArgs a) {
         resources(a.c.v, i, rows[st], rsrc);
         tile.request(rsrc, st * Shape::STAGE_B + Tile::TILE_B);
     };
+    // kShareKeys: wave 0 brings the first 16 rows of K of tile i, 1 the others, 2 and 3 those of V, and wave 0 the scales; `pending` takes
+    // which halves of it are on no page
+    int pending = 0;
+    const uint32_t src_shared = tile.src0 ^ (uint32_t)((wave & 1) << 4);
+    auto request_shared = [&](int i, uint32_t offset, int ahead) __attribute__((always_inline)) {
+        if ((i & 63) == 0 && i > 0) look_up(i);
+        const UniformRow lo(row_lo, i & 63), hi(row_hi, i & 63), row = wave & 1 ? hi : lo;
+        pending |= ((lo.none() & 1) | (hi.none() & 2)) << (2 * ahead);
+        const int there = key1 - (key0 + 32 * i);
+        int n = max(there - 16 * (wave & 1), 0);
+        asm volatile("" : "+s"(n));
+        n = min(n, 16) & ~row.none();
+        const BufferWords rsrc = make_buffer_words(static_cast<const char*>(wave & 2 ? a.c.v : a.c.k) + row.index() * Tile::ROWB, n * Tile::ROWB);
+        tile.request_half(rsrc, offset + (wave >> 1) * Tile::TILE_B + (wave & 1) * (Tile::TILE_B / 2), src_shared);
+        if constexpr (CODES)
+            if (wave == 0) {
+                long at_row = lo.index(), upper = hi.index();
+                asm volatile("" : "+v"(at_row), "+v"(upper));
+                at_row = lane & 16 ? upper : at_row;
+                const long at = (lane & 31) >= there ? 0 : at_row + (lane & 15);
+                global_to_lds_4B((lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + offset + 2 * Tile::TILE_B);
+            }
+    };
     int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
     i32x4 qreg[RT][QS];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const int row = min((rg * RT + x) * COLS + col, n_rows - 1), g = row / a.T;
+        const int row = min(((rg * RW + rw) * RT + x) * COLS + col, n_rows - 1), g = row / a.T;
         t[x] = row - g * a.T;
         const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (b * a.q.batch + (kvh * group + g) * a.q.head + t[x] * a.q.token);
 #pragma unroll
@@ -508,11 +523,17 @@ fa_fwd_cache_kernel(CachedArgs a) {
     for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int u = 0; u < QS; ++u) asm volatile("" : "+v"(qreg[x][u]));
-    if (mine > 0)
-        static_for<STG>([&](auto st) {
-            request_k(st, st);
-            request_v(st, st);
-        });
+    if (mine > 0) {
+        if constexpr (SHARED) {
+#pragma unroll
+            for (int i = 0; i < STG - 1; ++i) request_shared(i, i * Shape::STAGE_B, i);
+        } else {
+            static_for<STG>([&](auto st) {
+                request_k(st, st);
+                request_v(st, st);
+            });
+        }
+    }
 
     typename M::Acc acc[RT][NT];
     float m_run[RT], l_run[RT];
@@ -542,16 +563,11 @@ fa_fwd_cache_kernel(CachedArgs a) {
         return vis & live;
     };
 
-    for (int i0 = 0; i0 < mine; i0 += STG) {
-        static_for<STG>([&](auto stage) __attribute__((always_inline)) {
-            constexpr int st = decltype(stage)::value, kK = st * Shape::STAGE_B, kV = kK + Tile::TILE_B, kScales = kK + 2 * Tile::TILE_B;
-            const int i = i0 + st;
-            if (i >= mine) return;
-            const int key = key0 + 32 * (wave + NW * i), next = i + STG;
-            // the places of the tile that are there and on a page
-            const int bad = (rows[st][0].none() & 1) | (rows[st][1].none() & 2);
+    int odd = 0;  // whether V of a new token held a value that is not finite
+    // A tile: scores, softmax, products.  `at`: where it is (K, V, scales from OFFSET on); `bad`: the halves that are on no page
+    auto work = [&](const Tile& at, auto off, int key, int bad, auto&& after_scores, auto&& before_products, auto&& after_products) __attribute__((always_inline)) {
+            constexpr int kK = decltype(off)::value, kV = kK + Tile::TILE_B, kScales = kK + 2 * Tile::TILE_B;
             const bool special = key + 32 > min(ext.len, key1) || bad != 0;
-            wait_vmcnt<NI * STG + (NI + X) * (STG - 1)>();  // K has landed
             float s[RT][NS];
             {
                 typename M::Acc y[RT][M::TILES];
@@ -563,7 +579,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     constexpr int k = decltype(n)::value;
                     static_for<M::TILES>([&](auto m) __attribute__((always_inline)) {
                         constexpr int kt = decltype(m)::value;
-                        const i32x4 w = tile.template row_read<k, kt>(kK);
+                        const i32x4 w = at.template row_read<k, kt>(kK);
                         if constexpr (CODES) {
                             const i32x4 lo = from_codes<Tag>(w[0], w[1]), hi = from_codes<Tag>(w[2], w[3]);
 #pragma unroll
@@ -585,8 +601,8 @@ fa_fwd_cache_kernel(CachedArgs a) {
             if constexpr (CODES) {
 #pragma unroll
                 for (int g = 0; g < NS / 4; ++g) {
-                    const uint32_t at = tile.base + kScales + 4 * (M::bit(4 * g) + (part << M::SHIFT));
-                    const f32x4 ks = lds_load_4f(at), vs = lds_load_4f(at + 128);
+                    const uint32_t scales = at.base + kScales + 4 * (M::bit(4 * g) + (part << M::SHIFT));
+                    const f32x4 ks = lds_load_4f(scales), vs = lds_load_4f(scales + 128);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         vscale[4 * g + r] = vs[r];
@@ -595,8 +611,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     }
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K and the scales have been read: the next ones may come
-            request_k(next, stage);
+            after_scores();
 
             uint32_t seen[RT];
             if (special) {
@@ -672,31 +687,67 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                 for (int r = 0; r < NS; r += 2) pb[x][r >> 3][(r >> 1) & 3] = PE::pack2(s[x][r], s[x][r + 1]);
             }
-            wait_vmcnt<(NI + X) * STG + NI * (STG - 1)>();  // V has landed
+            before_products();
             if (special && key + 32 > ext.len)
-                if (__builtin_expect(tile.not_finite(kV, lane), 0)) {
-#pragma unroll
-                    for (int x = 0; x < RT; ++x) tile.add_not_finite(kV, seen[x], acc[x]);
-                    tile.clear_not_finite(kV, lane);
+                if (__builtin_expect(at.not_finite(kV, lane), 0)) {
+                    odd = 1;
+                    if constexpr (SHARED) barrier();  // all waves have seen it; then each clears all
+                    at.clear_not_finite(kV, lane);
                 }
             // O^T += V^T P^T
             static_for<M::SLABS>([&](auto sl) __attribute__((always_inline)) {
                 static_for<NT>([&](auto d) __attribute__((always_inline)) {
                     constexpr int slab = decltype(sl)::value, dt = decltype(d)::value;
-                    i32x4 w = tile.template columns<dt, slab>(kV);
+                    i32x4 w = at.template columns<dt, slab>(kV);
                     if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
 #pragma unroll
                     for (int x = 0; x < RT; ++x) acc[x][dt] = PM::mma(w, pb[x][slab], acc[x][dt]);
                 });
             });
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            request_v(next, stage);
-        });
+            after_products();
+    };
+    if constexpr (SHARED) {
+        // Tile i + STG - 1 goes where tile i - 1 was, which all waves have left when they meet in tile i
+        uint32_t now_at = 0, next_at = (STG - 1) * Shape::STAGE_B;
+        for (int i = 0; i < mine; ++i) {
+            wait_vmcnt<(STG - 2) * (NI / 2)>();  // what this wave brings of tile i has landed
+            barrier();
+            request_shared(i + STG - 1, next_at, STG - 1);
+            Tile at = tile;
+            at.base += now_at;
+            at.row0 += now_at;
+            at.tr0 += now_at;
+            work(at, std::integral_constant<int, 0>{}, key0 + 32 * i, pending & 3, [] {}, [] {}, [] {});
+            pending >>= 2;
+            next_at = now_at;
+            now_at = now_at == (STG - 1) * Shape::STAGE_B ? 0 : now_at + Shape::STAGE_B;
+        }
+    } else {
+        for (int i0 = 0; i0 < mine; i0 += STG)
+            static_for<STG>([&](auto stage) __attribute__((always_inline)) {
+                constexpr int st = decltype(stage)::value;
+                const int i = i0 + st;
+                if (i >= mine) return;
+                const int bad = (rows[st][0].none() & 1) | (rows[st][1].none() & 2);
+                wait_vmcnt<NI * STG + (NI + X) * (STG - 1)>();  // K has landed
+                work(tile, std::integral_constant<int, st * Shape::STAGE_B>{}, key0 + 32 * (kw + KW * i), bad,
+                     [&] {
+                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K and the scales have been read: the next ones may come
+                         request_k(i + STG, stage);
+                     },
+                     [&] { wait_vmcnt<(NI + X) * STG + NI * (STG - 1)>(); },  // V has landed
+                     [&] {
+                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                         request_v(i + STG, stage);
+                     });
+            });
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last requests: the LDS is about to be reused
 
-    // The waves' states meet: with M the largest reference and f = 2^(m - M), sum f F acc, M and sum f l
+    // The states of waves that divided the keys meet: with M the largest reference and f = 2^(m - M), sum f F acc, M and sum f l
     float* const state = reinterpret_cast<float*>(lds + Shape::LDS - Shape::STATE_B);  // [RT][NW][COLS][m, l, F]
+    int* const odd_waves = reinterpret_cast<int*>(state + NW * COLS * RT * 3);
+    if (lane == 0) odd_waves[wave] = odd;
     float* const merge = reinterpret_cast<float*>(lds);                                // [NW][COLS][MERGE_STRIDE]
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
@@ -723,30 +774,49 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     *reinterpret_cast<f32x4*>(merge + (wave * COLS + col) * MS + dt * M::WIDTH - c0 + 4 * M::PARTS * g + 4 * part) = w;
                 }
             __syncthreads();
-            for (int c = tid; c < COLS * MC / 8; c += NW * 64) {
-                const int r = c / (MC / 8), cc = (c % (MC / 8)) * 8, row = (rg * RT + x) * COLS + r;
+            for (int c = SHARED ? lane : tid; c < COLS * MC / 8; c += KW * 64) {
+                const int r = c / (MC / 8), cc = (c % (MC / 8)) * 8, row = ((rg * RW + rw) * RT + x) * COLS + r;
                 if (row >= n_rows) continue;
                 const int g = row / a.T, tok = row - g * a.T;
                 if (tok >= ext.count) continue;
-                float m_all = -INFINITY, l_all = 0.f, f[NW];
+                float m_all = -INFINITY, l_all = 0.f, f[KW];
 #pragma unroll
-                for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, state[((x * NW + w) * COLS + r) * 3]);
+                for (int w = 0; w < KW; ++w) m_all = fmaxf(m_all, state[((x * NW + rw + w) * COLS + r) * 3]);
                 const float m_ref = m_all == -INFINITY ? 0.f : m_all;
 #pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    const float* at = state + ((x * NW + w) * COLS + r) * 3;
+                for (int w = 0; w < KW; ++w) {
+                    const float* at = state + ((x * NW + rw + w) * COLS + r) * 3;
                     f[w] = fast_exp2(at[0] - m_ref);
                     l_all += f[w] * at[1];
                     f[w] *= at[2];
                 }
                 float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int w = 0; w < NW; ++w)
+                for (int w = 0; w < KW; ++w)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const f32x4 z = *reinterpret_cast<const f32x4*>(merge + (w * COLS + r) * MS + cc + 4 * h);
+                        const f32x4 z = *reinterpret_cast<const f32x4*>(merge + ((rw + w) * COLS + r) * MS + cc + 4 * h);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[4 * h + e] = __builtin_fmaf(f[w], z[e], y[4 * h + e]);
+                    }
+                int any_odd = 0;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) any_odd |= odd_waves[rw + w];
+                if (__builtin_expect(any_odd != 0, 0))
+                    for (int u = max(key0 - ext.len, 0); u < key1 - ext.len; ++u) {  // new tokens of these keys that the row sees
+                        const int place = ext.len + u, entry = place / a.c.page_size, words = (a.T + 31) >> 5;
+                        const bool sees = a.tree ? a.tree[((long)(a.tree_batches == 1 ? 0 : b) * a.T + tok) * words + (u >> 5)] >> (u & 31) & 1 : u <= tok;
+                        const int page = a.c.block_table[(long)b * a.c.max_pages + entry];
+                        if (!sees || page < 0 || page >= a.c.n_pages) continue;
+                        const long at = (((long)page * H_kv + kvh) * a.c.page_size + (place - entry * a.c.page_size)) * D + c0 + cc;
+                        for (int e = 0; e < 8; ++e) {
+                            float v;
+                            if constexpr (CODES) v = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(a.c.v)[at + e], 0);
+                            else v = E::to_float(static_cast<const uint16_t*>(a.c.v)[at + e]);
+                            if (!(fabsf(v) < INFINITY))
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) y[k] += k == e ? v : 0.f;
+                        }
                     }
                 if (whole) {
                     const int head = kvh * group + g;
@@ -758,7 +828,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     *reinterpret_cast<i32x4*>(o + c0 + cc) = w;
                     if (c0 + cc == 0) a.lse[((long)b * a.H + head) * a.T + tok] = (m_all + log2f(l_all)) * kLn2;
                 } else {
-                    const long at = ((long)wg * 2 + segment) * Shape::ROWS + x * COLS + r;
+                    const long at = ((long)wg * 2 + segment) * Shape::ROWS + (rw * RT + x) * COLS + r;
                     float* o = a.part + at * D + c0 + cc;
                     *reinterpret_cast<f32x4*>(o) = f32x4{y[0], y[1], y[2], y[3]};
                     *reinterpret_cast<f32x4*>(o + 4) = f32x4{y[4], y[5], y[6], y[7]};
@@ -867,8 +937,8 @@ __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
 #endif
 constexpr int kWaves = 4;
 // How deep a wave stages: as the LDS of a CU allows with as many workgroups as its registers do
-template <typename Tag, int D, bool CODES, int COLS, int RT>
-using CachedForm = CachedShape<Tag, D, CODES, COLS, RT, kWaves, (D * (CODES ? 1 : 2) <= 128 ? 2 : X_STG)>;
+template <typename Tag, int D, bool CODES, int COLS, int RT, int FORM>
+using CachedForm = CachedShape<Tag, D, CODES, COLS, RT, kWaves, (FORM == kShareKeys ? 3 : D * (CODES ? 1 : 2) <= 128 ? 2 : X_STG), FORM>;
 
 // Calls f with the shape that a call takes
 template <typename F>
@@ -876,10 +946,15 @@ static auto with_shape(int rows, int d, bool codes, F&& f) {
     auto by_rows = [&](auto D, auto c) {
         constexpr int d_ = decltype(D)::value;
         constexpr bool c_ = decltype(c)::value;
-        if (rows <= 16) return f(CachedForm<bf16_tag, d_, c_, 16, 1>{}, D, c, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+        auto go = [&](auto cols, auto rt, auto form) {
+            return f(CachedForm<bf16_tag, d_, c_, decltype(cols)::value, decltype(rt)::value, decltype(form)::value>{}, D, c, cols, rt, form);
+        };
+        using std::integral_constant;
+        if (rows <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{}, integral_constant<int, kDivideKeys>{});
+        if (rows > X_ROWS) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{}, integral_constant<int, kShareKeys>{});
         if constexpr (d_ < 256)
-            if (rows > 32) return f(CachedForm<bf16_tag, d_, c_, 32, 2>{}, D, c, std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
-        return f(CachedForm<bf16_tag, d_, c_, 32, 1>{}, D, c, std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+            if (rows > 32) return go(integral_constant<int, 32>{}, integral_constant<int, 2>{}, integral_constant<int, kDivideKeys>{});
+        return go(integral_constant<int, 32>{}, integral_constant<int, 1>{}, integral_constant<int, kDivideKeys>{});
     };
     auto by_codes = [&](auto D) { return codes ? by_rows(D, std::true_type{}) : by_rows(D, std::false_type{}); };
     switch (d) {
@@ -906,7 +981,7 @@ struct CachedDivision {
     size_t bytes(int d) const { return teams == 0 ? 0 : table_bytes + rows * (d + 2) * sizeof(float); }
 };
 
-template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT>
+template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT, int FORM>
 static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t stream) {
     CachedDivision div(Shape{}, a.B, a.H, a.c.H_kv, a.T, max_len);
     // (steps are counted in 32 bits, and there may be as many as there are places, whatever was expected)
@@ -920,8 +995,8 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
     }
     const double total = (double)(div.teams != 0 ? div.teams : (double)a.B * a.c.H_kv) * a.row_groups;
     if (total * 64 * kWaves >= 4294967296.0) return FA_ERR_LAUNCH;
-    constexpr int STG = Shape::WAVE_B / Shape::STAGE_B;
-    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, CODES, COLS, RT, kWaves, STG>), dim3((unsigned)total), dim3(kWaves * 64), Shape::LDS, stream, a);
+    constexpr int STG = Shape::STAGES_B / Shape::STAGE_B / (FORM == kShareKeys ? 1 : kWaves);
+    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, CODES, COLS, RT, kWaves, STG, FORM>), dim3((unsigned)total), dim3(kWaves * 64), Shape::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     if (div.teams != 0) {
         const long rows = (long)a.B * a.H * a.T;
@@ -942,12 +1017,12 @@ size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_l
 int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
                      void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream) {
     const CachedArgs a = {q, o, cache, counts, tree, lse, nullptr, nullptr, nullptr, B, H, T, tree_batches, 1, 0, scale};
-    return with_shape(H / cache.H_kv * T, d, cache.dtype == FA_FP8_E4M3, [&](auto shape, auto D, auto codes, auto cols, auto rt) {
+    return with_shape(H / cache.H_kv * T, d, cache.dtype == FA_FP8_E4M3, [&](auto shape, auto D, auto codes, auto cols, auto rt, auto form) {
         using Shape = decltype(shape);
-        constexpr int d_ = decltype(D)::value, cols_ = decltype(cols)::value, rt_ = decltype(rt)::value;
+        constexpr int d_ = decltype(D)::value, cols_ = decltype(cols)::value, rt_ = decltype(rt)::value, form_ = decltype(form)::value;
         constexpr bool codes_ = decltype(codes)::value;
-        return dtype == FA_BF16 ? launch_cached<bf16_tag, Shape, d_, codes_, cols_, rt_>(a, workspace, max_len, stream)
-                                : launch_cached<f16_tag, Shape, d_, codes_, cols_, rt_>(a, workspace, max_len, stream);
+        return dtype == FA_BF16 ? launch_cached<bf16_tag, Shape, d_, codes_, cols_, rt_, form_>(a, workspace, max_len, stream)
+                                : launch_cached<f16_tag, Shape, d_, codes_, cols_, rt_, form_>(a, workspace, max_len, stream);
     });
 }
 
