@@ -185,10 +185,15 @@ struct CacheTile {
     static constexpr int ROWB = D * (CODES ? 1 : 2), TILE_B = 32 * ROWB, CPR = ROWB / 16, RPI = 1024 / ROWB, NI = 32 / RPI;
     static constexpr int MASK = CPR < 16 ? CPR - 1 : 15;
     static constexpr int KR = CPR / M::PARTS;  // row reads of a lane and score tile
+    // KEPT (32 columns, where matrix and vector instructions compete): an address register for each chunk instead, the rest in
+    // the instructions' offsets; the 16 rows of the other slab have the same swizzle
+    static constexpr bool KEPT = COLS == 32;
+    static constexpr int TR = CODES ? 1 : 2;
     uint32_t base, src0, row0, tr0;
+    uint32_t row_at[KEPT ? KR : 1], tr_at[KEPT ? M::NT : 1][TR];
 
     static constexpr __device__ __host__ int swizzle(int r) {
-        return ((r & 1) << 3 | (r >> 1 & 1) << 2 | (r >> 3 & 1) << 1 | ((r >> 2 ^ r >> 4) & 1)) & MASK;
+        return ((r & 1) << 3 | (r >> 1 & 1) << 2 | (r >> 3 & 1) << 1 | ((COLS == 16 ? r >> 2 ^ r >> 4 : r >> 2) & 1)) & MASK;
     }
     // what bringing chunk c into an address of row r, or adding row bits that r has not, does to it
     static constexpr __device__ uint32_t flip(int chunk, int more_rows) { return (uint32_t)((chunk & MASK) ^ swizzle(more_rows)) << 4; }
@@ -208,6 +213,22 @@ struct CacheTile {
             tr0 = at + tr * ROWB + (((COLS == 32 ? 2 * blk : 0) + (quad >> 1)) ^ swizzle(tr)) * 16 + 8 * (quad & 1);
         }
         asm volatile("" : "+v"(src0), "+v"(row0), "+v"(tr0));
+        if constexpr (KEPT) {
+            static_for<KR>([&](auto n) __attribute__((always_inline)) {
+                constexpr int k = decltype(n)::value;
+                row_at[k] = (row0 ^ flip(M::PARTS * k, 0)) + plus(M::PARTS * k, 0);
+                asm volatile("" : "+v"(row_at[k]));
+            });
+            static_for<M::NT>([&](auto n) __attribute__((always_inline)) {
+                constexpr int dt = decltype(n)::value, chunk = (CODES ? 2 : 4) * dt;
+                tr_at[dt][0] = (tr0 ^ flip(chunk, 0)) + plus(chunk, 0);
+                asm volatile("" : "+v"(tr_at[dt][0]));
+                if constexpr (!CODES) {
+                    tr_at[dt][TR - 1] = (tr0 ^ flip(chunk, 8)) + plus(chunk, 8);
+                    asm volatile("" : "+v"(tr_at[dt][TR - 1]));
+                }
+            });
+        }
     }
     // All instructions that bring a tile, 16 rows from each resource
     __device__ __forceinline__ void request(const BufferWords (&rsrc)[2], uint32_t offset) const {
@@ -226,12 +247,19 @@ struct CacheTile {
     // the lane's 16 bytes k of its row in score tile kt
     template <int K, int KT>
     __device__ __forceinline__ i32x4 row_read(uint32_t offset) const {
-        return lds_load_16B((row0 ^ flip(M::PARTS * K, 4 * KT)) + (offset + plus(M::PARTS * K, 4 * KT)));
+        if constexpr (KEPT) return lds_load_16B(row_at[K] + offset);
+        else return lds_load_16B((row0 ^ flip(M::PARTS * K, 4 * KT)) + (offset + plus(M::PARTS * K, 4 * KT)));
     }
     // the A operand of V^T: accumulator dt, keys of slab `slab`; codes: their eight bytes
     template <int DT, int SLAB>
     __device__ __forceinline__ i32x4 columns(uint32_t offset) const {
-        if constexpr (CODES) {
+        if constexpr (KEPT && CODES) {
+            const i32x2 c = lds_read_tr8(tr_at[DT][0] + (offset + SLAB * 16 * ROWB));
+            return i32x4{c[0], c[1], 0, 0};
+        } else if constexpr (KEPT) {
+            const i32x2 lo = lds_read_tr16(tr_at[DT][0] + (offset + SLAB * 16 * ROWB)), hi = lds_read_tr16(tr_at[DT][TR - 1] + (offset + SLAB * 16 * ROWB));
+            return i32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else if constexpr (CODES) {
             constexpr int chunk = COLS == 32 ? 2 * DT : DT;
             const i32x2 c = lds_read_tr8((tr0 ^ flip(chunk, 16 * SLAB)) + (offset + plus(chunk, 16 * SLAB)));
             return i32x4{c[0], c[1], 0, 0};
@@ -350,7 +378,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     int team = xcd_run(blockIdx.x, gridDim.x);
     const int wg = team, rg = __builtin_amdgcn_readfirstlane(team % a.row_groups);
     team = __builtin_amdgcn_readfirstlane(team / a.row_groups);
-    const int H_kv = a.c.H_kv, group = a.H / H_kv, n_rows = group * a.T;
+    const int H_kv = a.c.H_kv, group = a.H / H_kv;
     int b, kvh, step = 0, left = 0x7fffffff;  // the first segment, and how many steps the team has
     Extent ext;
     uint32_t pos = 0;  // of the team's first step among all
@@ -429,7 +457,9 @@ fa_fwd_cache_kernel(CachedArgs a) {
     const int now = min(n_steps - step, left);
     const bool whole = now == n_steps;
     const int key0 = step * Shape::STEP, key1 = step + now == n_steps ? ext.keys : key0 + now * Shape::STEP;
-    const int n_tiles = (int)(((unsigned)max(key1 - key0, 0) + 31) / 32), mine = n_tiles > kw ? (n_tiles - kw + KW - 1) / KW : 0;
+    // rows of the tokens that are there, packed; a team's last workgroups may have none
+    const int n_rows = group * ext.count, per = max(ext.count, 1);
+    const int n_tiles = rg * Shape::ROWS >= n_rows ? 0 : (int)(((unsigned)max(key1 - key0, 0) + 31) / 32), mine = n_tiles > kw ? (n_tiles - kw + KW - 1) / KW : 0;
 
     // rows (of all pages' rows, heads included) of the wave's tiles: lane i has tile i of 64, two times 16 places; -1: no page
     long row_lo = -1, row_hi = -1;
@@ -483,7 +513,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // kShareKeys: wave 0 brings the first 16 rows of K of tile i, 1 the others, 2 and 3 those of V, and wave 0 the scales; `pending` takes
     // which halves of it are on no page
     int pending = 0;
-    const uint32_t src_shared = tile.src0 ^ (uint32_t)((wave & 1) << 4);
+    const uint32_t src_shared = tile.src0 ^ (uint32_t)((wave & 1) * (Tile::swizzle(16) << 4));
     auto request_shared = [&](int i, uint32_t offset, int ahead) __attribute__((always_inline)) {
         if ((i & 63) == 0 && i > 0) look_up(i);
         const UniformRow lo(row_lo, i & 63), hi(row_hi, i & 63), row = wave & 1 ? hi : lo;
@@ -507,8 +537,8 @@ fa_fwd_cache_kernel(CachedArgs a) {
     i32x4 qreg[RT][QS];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const int row = min(((rg * RW + rw) * RT + x) * COLS + col, n_rows - 1), g = row / a.T;
-        t[x] = row - g * a.T;
+        const int row = min(((rg * RW + rw) * RT + x) * COLS + col, max(n_rows - 1, 0)), g = row / per;
+        t[x] = row - g * per;
         const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (b * a.q.batch + (kvh * group + g) * a.q.head + t[x] * a.q.token);
 #pragma unroll
         for (int u = 0; u < QS; ++u) {
@@ -708,20 +738,17 @@ fa_fwd_cache_kernel(CachedArgs a) {
     };
     if constexpr (SHARED) {
         // Tile i + STG - 1 goes where tile i - 1 was, which all waves have left when they meet in tile i
-        uint32_t now_at = 0, next_at = (STG - 1) * Shape::STAGE_B;
-        for (int i = 0; i < mine; ++i) {
-            wait_vmcnt<(STG - 2) * (NI / 2)>();  // what this wave brings of tile i has landed
-            barrier();
-            request_shared(i + STG - 1, next_at, STG - 1);
-            Tile at = tile;
-            at.base += now_at;
-            at.row0 += now_at;
-            at.tr0 += now_at;
-            work(at, std::integral_constant<int, 0>{}, key0 + 32 * i, pending & 3, [] {}, [] {}, [] {});
-            pending >>= 2;
-            next_at = now_at;
-            now_at = now_at == (STG - 1) * Shape::STAGE_B ? 0 : now_at + Shape::STAGE_B;
-        }
+        for (int i0 = 0; i0 < mine; i0 += STG)
+            static_for<STG>([&](auto stage) __attribute__((always_inline)) {
+                constexpr int st = decltype(stage)::value;
+                const int i = i0 + st;
+                if (i >= mine) return;
+                wait_vmcnt<(STG - 2) * (NI / 2)>();  // what this wave brings of tile i has landed
+                barrier();
+                request_shared(i + STG - 1, (st + STG - 1) % STG * Shape::STAGE_B, STG - 1);
+                work(tile, std::integral_constant<int, st * Shape::STAGE_B>{}, key0 + 32 * i, pending & 3, [] {}, [] {}, [] {});
+                pending >>= 2;
+            });
     } else {
         for (int i0 = 0; i0 < mine; i0 += STG)
             static_for<STG>([&](auto stage) __attribute__((always_inline)) {
@@ -777,8 +804,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
             for (int c = SHARED ? lane : tid; c < COLS * MC / 8; c += KW * 64) {
                 const int r = c / (MC / 8), cc = (c % (MC / 8)) * 8, row = ((rg * RW + rw) * RT + x) * COLS + r;
                 if (row >= n_rows) continue;
-                const int g = row / a.T, tok = row - g * a.T;
-                if (tok >= ext.count) continue;
+                const int g = row / per, tok = row - g * per;
                 float m_all = -INFINITY, l_all = 0.f, f[KW];
 #pragma unroll
                 for (int w = 0; w < KW; ++w) m_all = fmaxf(m_all, state[((x * NW + rw + w) * COLS + r) * 3]);
@@ -869,9 +895,9 @@ __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
     const unsigned n_rows = (unsigned)a.B * a.H * a.T, row = blockIdx.x * (GROUPS / ways) + group / ways;
     const unsigned bh = min(row, n_rows - 1) / a.T;
     const int tok = row - bh * a.T, b = bh / (unsigned)a.H, head = bh - b * a.H;
-    const int heads = a.H / a.c.H_kv, kvh = head / heads, in_group = (head - kvh * heads) * a.T + tok, rg = in_group / ROWS;
+    const int heads = a.H / a.c.H_kv, kvh = head / heads, count = a.counts ? min(a.counts[b], a.T) : a.T;
+    const int in_group = (head - kvh * heads) * count + tok, rg = in_group / ROWS;
     const CachedArgs::Segments of = a.segments[b * a.c.H_kv + kvh];
-    const int count = a.counts ? a.counts[b] : a.T;
     const bool there = row < n_rows && of.count > 1 && tok < count;
     float m = -INFINITY, l = 0.f;
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
