@@ -24,18 +24,6 @@
 //     instructions for a tile.
 #include "fa_device.h"
 #include "fa_launch.h"
-#ifndef X_ROWS
-#define X_ROWS 64
-#endif
-#ifndef X_S64
-#define X_S64 3
-#endif
-#ifndef X_S128
-#define X_S128 2
-#endif
-#ifndef X_SHLOAD
-#define X_SHLOAD global_to_lds_16B
-#endif
 
 namespace fa {
 
@@ -162,12 +150,9 @@ template <typename Tag, int D> struct Matrix<Tag, D, 16> {
     }
 };
 
-#ifndef X_NT
-#define X_NT " nt"
-#endif
 // global_to_lds_16B of what nobody else reads
 static __device__ __forceinline__ void once_to_lds_16B(const BufferWords& rsrc, uint32_t lds_base, int byte_off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen" X_NT " lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
                  :
                  : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(byte_off), "s"(rsrc.w)
                  : "memory", "m0");
@@ -241,7 +226,7 @@ struct CacheTile {
     __device__ __forceinline__ void request_half(const BufferWords& rsrc, uint32_t offset, uint32_t src) const {
         static_for<NI / 2>([&](auto n) __attribute__((always_inline)) {
             constexpr int i = decltype(n)::value, r = i * RPI;
-            X_SHLOAD(rsrc, base + offset + i * 1024, (int)((src ^ (uint32_t)(swizzle(r) << 4)) + r * ROWB));
+            global_to_lds_16B(rsrc, base + offset + i * 1024, (int)((src ^ (uint32_t)(swizzle(r) << 4)) + r * ROWB));
         });
     }
     // the lane's 16 bytes k of its row in score tile kt
@@ -352,7 +337,7 @@ struct CachedShape {
     static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 3 * 4 + NW * 4;
     static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
     // workgroups (of four waves) to a CU, by registers
-    static constexpr int WAVES = SHARED ? (D == 64 ? X_S64 : D == 128 ? X_S128 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
+    static constexpr int WAVES = SHARED ? (D == 64 ? 3 : D == 128 ? 2 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
     static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;
 };
 
@@ -369,6 +354,9 @@ fa_fwd_cache_kernel(CachedArgs a) {
     using E = Elem<Tag>;
     constexpr int NS = M::NS, NT = M::NT, NI = Tile::NI, X = CODES ? 1 : 0, ACC = sizeof(typename M::Acc) / 4;
     constexpr bool ACCUMULATION = Shape::WAVES == 1;  // more than 256 registers: accumulators in the half for matrix results
+    // Few rows leave the matrix pipes idle: P goes in as its rounded value and what that leaves out, so that its rounding does not
+    // add to the output's (error against 64 bits, bf16, of the output's rounding alone: 1.4 times / 1.0 times; the time is the same)
+    constexpr bool TWO_PARTS = COLS == 16;
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -681,7 +669,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                 for (int r = 0; r < NS; ++r) vscale[r] *= inv_F;
             }
-            i32x4 pb[RT][M::SLABS];  // what V is multiplied by
+            i32x4 pb[RT][M::SLABS], rest[RT][M::SLABS];  // what V is multiplied by
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -715,7 +703,13 @@ fa_fwd_cache_kernel(CachedArgs a) {
                         for (int r = 0; r < NS; ++r) s[x][r] = seen[x] >> M::bit(r) & 1 ? s[x][r] : 0.f;
                 l_run[x] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
 #pragma unroll
-                for (int r = 0; r < NS; r += 2) pb[x][r >> 3][(r >> 1) & 3] = PE::pack2(s[x][r], s[x][r + 1]);
+                for (int r = 0; r < NS; r += 2) {
+                    const int w = PE::pack2(s[x][r], s[x][r + 1]);
+                    pb[x][r >> 3][(r >> 1) & 3] = w;
+                    if constexpr (TWO_PARTS)
+                        rest[x][r >> 3][(r >> 1) & 3] =
+                            PE::pack2(s[x][r] - PE::to_float((uint16_t)w), s[x][r + 1] - PE::to_float((uint16_t)((uint32_t)w >> 16)));
+                }
             }
             before_products();
             if (special && key + 32 > ext.len)
@@ -731,7 +725,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     i32x4 w = at.template columns<dt, slab>(kV);
                     if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) acc[x][dt] = PM::mma(w, pb[x][slab], acc[x][dt]);
+                    for (int x = 0; x < RT; ++x) {
+                        acc[x][dt] = PM::mma(w, pb[x][slab], acc[x][dt]);
+                        if constexpr (TWO_PARTS) acc[x][dt] = PM::mma(w, rest[x][slab], acc[x][dt]);
+                    }
                 });
             });
             after_products();
@@ -952,35 +949,54 @@ __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
     if (c == 0) a.lse[row] = (m + log2f(l)) * kLn2;
 }
 
-#ifndef X_JOIN
-#define X_JOIN 256
-#endif
-#ifndef X_OVER
-#define X_OVER 1
-#endif
-#ifndef X_STG
-#define X_STG 1
-#endif
-constexpr int kWaves = 4;
-// How deep a wave stages: as the LDS of a CU allows with as many workgroups as its registers do
-template <typename Tag, int D, bool CODES, int COLS, int RT, int FORM>
-using CachedForm = CachedShape<Tag, D, CODES, COLS, RT, kWaves, (FORM == kShareKeys ? 3 : D * (CODES ? 1 : 2) <= 128 ? 2 : X_STG), FORM>;
+// Whether each workgroup has a whole sequence and head: one launch, and nothing is looked for or joined, but the longest sequence
+// decides.  So up to a length that goes with the workgroups there are (where they fill the chip anyway, any), in keys that take as
+// long as those of 16 rows at d = 128.  us, whole / teams, by workgroups and the longest of lengths spread over its last third
+// (T = 1) or half, bf16:
+//   T = 1 d = 64   8: 768 8.9 / 10.5, 1536 12.7 / 10.9;  128: 1536 15.0 / 15.3;  256: 3000 29.5 / 34.2;  512: 4500 79 / 84
+//         d = 128  8: 512 9.5 / 11.4, 1024 13.1 / 11.7;  128: 1024 16.1 / 17.5;  256: 3000 55 / 59, but spread from a tenth of it on
+//                  4096 55.6 / 51.5;  512: 4500 155 / 160
+//   32 rows        32: 1024 16.0 / 16.7;  128: 2048 28 / 29;  256: 4500 77 / 84.   64 rows  64: 768 21.0 / 20.8;  128: 2048 35 / 38
+//   256 rows       128: 512 25.9 / 28.3, 768 32 / 30;  256: 1024 41 / 46, 2048 66 / 59;  512: 4500 157 / 166
+template <typename Form>
+static bool whole_sequences(double workgroups, int max_len) {
+    constexpr bool shared = Form::FORM == kShareKeys;
+    constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
+                     d256 = Form::COLS == 16 ? (Form::CODES ? 1.5 : 2.0) : shared ? 2.0 : 1.25;
+    if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return true;
+    const double limit = 8 * workgroups + 256 > 512 ? 8 * workgroups + 256 : 512;
+    return max_len * (Form::D == 64 ? d64 : Form::D == 128 ? d128 : d256) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
+}
 
-// Calls f with the shape that a call takes
+// Calls f with the shape that a call takes, and what its template arguments are.  (The shapes do not depend on the 16-bit type.)
+//   rows to a key/value head  up to 16: 16 columns; 17 to 32: 32; 33 to 64: two tiles of 32 to a wave, so that each operand is read once for
+//   both; more: four tiles, a wave each, that share what is staged (256 rows 94 us, divided keys 115; 52 rows 27.4 and 25.9).
+// Eight waves instead of four halve the chain of a sequence that a workgroup has for itself, where its keys are small enough for two
+// such workgroups' worth of LDS to be worth it: us, four / eight, T = 1, 8 heads: d = 64 1024 10.1 / 8.6; codes d = 128 768 13.0 / 10.6,
+// d = 256 512 15.7 / 13.7; bf16 d = 128 768 11.2 / 10.3 but 2048 22.2 / 21.7, and 300 7.5 / 7.7.
+template <int D_, bool CODES_, int COLS_, int RT_, int NW_, int FORM_>
+struct CachedForm {
+    static constexpr int D = D_, COLS = COLS_, RT = RT_, NW = NW_, FORM = FORM_, STG = FORM == kShareKeys ? 3 : 1;
+    static constexpr bool CODES = CODES_;
+    template <typename Tag>
+    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>;
+};
 template <typename F>
-static auto with_shape(int rows, int d, bool codes, F&& f) {
+static auto with_form(int B, int H_kv, int rows, int d, int max_len, bool codes, F&& f) {
     auto by_rows = [&](auto D, auto c) {
         constexpr int d_ = decltype(D)::value;
         constexpr bool c_ = decltype(c)::value;
-        auto go = [&](auto cols, auto rt, auto form) {
-            return f(CachedForm<bf16_tag, d_, c_, decltype(cols)::value, decltype(rt)::value, decltype(form)::value>{}, D, c, cols, rt, form);
-        };
-        using std::integral_constant;
-        if (rows <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{}, integral_constant<int, kDivideKeys>{});
-        if (rows > X_ROWS) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{}, integral_constant<int, kShareKeys>{});
+        if (rows <= 16) {
+            if constexpr (d_ == 64 || c_) {
+                using Eight = CachedForm<d_, c_, 16, 1, 8, kDivideKeys>;
+                if ((double)B * H_kv <= (c_ && d_ == 128 ? 256 : 128) && max_len > 256 && whole_sequences<Eight>((double)B * H_kv, max_len)) return f(Eight{});
+            }
+            return f(CachedForm<d_, c_, 16, 1, 4, kDivideKeys>{});
+        }
+        if (rows > 64) return f(CachedForm<d_, c_, 32, 1, 4, kShareKeys>{});
         if constexpr (d_ < 256)
-            if (rows > 32) return go(integral_constant<int, 32>{}, integral_constant<int, 2>{}, integral_constant<int, kDivideKeys>{});
-        return go(integral_constant<int, 32>{}, integral_constant<int, 1>{}, integral_constant<int, kDivideKeys>{});
+            if (rows > 32) return f(CachedForm<d_, c_, 32, 2, 4, kDivideKeys>{});
+        return f(CachedForm<d_, c_, 32, 1, 4, kDivideKeys>{});
     };
     auto by_codes = [&](auto D) { return codes ? by_rows(D, std::true_type{}) : by_rows(D, std::false_type{}); };
     switch (d) {
@@ -990,26 +1006,29 @@ static auto with_shape(int rows, int d, bool codes, F&& f) {
     }
 }
 
-// How a call is divided.  (The shapes do not depend on the 16-bit type.)
+// How a call is divided.
 struct CachedDivision {
     int row_groups, teams;
     size_t table_bytes, rows;  // of the workspace: where segments are; the segments' rows
-    template <typename Shape>
-    CachedDivision(const Shape&, int B, int H, int H_kv, int T, int max_len) {
+    template <typename Form>
+    CachedDivision(const Form&, int B, int H, int H_kv, int T, int max_len) {
+        using Shape = typename Form::template Shape<bf16_tag>;
         row_groups = (H / H_kv * T + Shape::ROWS - 1) / Shape::ROWS;
-        const long items = (long)B * H_kv, most = ((long)max_len + Shape::STEP - 1) / Shape::STEP, slots = 256 * Shape::PER_CU * X_OVER;
+        const long items = (long)B * H_kv, most = ((long)max_len + Shape::STEP - 1) / Shape::STEP, slots = 256 * Shape::PER_CU;
         long n = slots / row_groups > 1 ? slots / row_groups : 1;
         if ((double)items * most < n) n = items * most;
-        teams = most <= 4 || items * row_groups >= 4 * slots ? 0 : (int)n;
+        teams = whole_sequences<Form>((double)items * row_groups, max_len) ? 0 : (int)n;
         table_bytes = ((size_t)items * sizeof(CachedArgs::Segments) + 15) / 16 * 16;
         rows = (size_t)teams * row_groups * 2 * Shape::ROWS;
     }
     size_t bytes(int d) const { return teams == 0 ? 0 : table_bytes + rows * (d + 2) * sizeof(float); }
 };
 
-template <typename Tag, typename Shape, int D, bool CODES, int COLS, int RT, int FORM>
+template <typename Tag, typename Form>
 static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t stream) {
-    CachedDivision div(Shape{}, a.B, a.H, a.c.H_kv, a.T, max_len);
+    using Shape = typename Form::template Shape<Tag>;
+    constexpr int D = Form::D, NW = Form::NW;
+    CachedDivision div(Form{}, a.B, a.H, a.c.H_kv, a.T, max_len);
     // (steps are counted in 32 bits, and there may be as many as there are places, whatever was expected)
     if ((double)a.B * a.c.H_kv * ((double)a.c.max_pages * a.c.page_size / Shape::STEP + 1) >= 2147483647.0) div.teams = 0;
     a.row_groups = div.row_groups;
@@ -1020,14 +1039,13 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
         a.state = a.part + div.rows * D;
     }
     const double total = (double)(div.teams != 0 ? div.teams : (double)a.B * a.c.H_kv) * a.row_groups;
-    if (total * 64 * kWaves >= 4294967296.0) return FA_ERR_LAUNCH;
-    constexpr int STG = Shape::STAGES_B / Shape::STAGE_B / (FORM == kShareKeys ? 1 : kWaves);
-    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, CODES, COLS, RT, kWaves, STG, FORM>), dim3((unsigned)total), dim3(kWaves * 64), Shape::LDS, stream, a);
+    if (total * 64 * NW >= 4294967296.0) return FA_ERR_LAUNCH;
+    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, Form::CODES, Form::COLS, Form::RT, NW, Form::STG, Form::FORM>), dim3((unsigned)total), dim3(NW * 64), Shape::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     if (div.teams != 0) {
         const long rows = (long)a.B * a.H * a.T;
         int ways = 1;  // the fewer rows there are, the more threads to a row
-        while (ways < 32 && ways < div.teams && rows * ways < 32 * X_JOIN) ways *= 2;
+        while (ways < 32 && ways < div.teams && rows * ways < 32 * 256) ways *= 2;
         hipLaunchKernelGGL((fa_join_kernel<Tag, D, Shape::ROWS>), dim3((unsigned)((rows * ways + 31) / 32), D / kJoinCols), dim3(256), 0, stream, a, ways);
         if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     }
@@ -1037,18 +1055,16 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
 }  // namespace
 
 size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype) {
-    return with_shape(H / H_kv * T, d, cache_dtype == FA_FP8_E4M3, [&](auto shape, auto...) { return CachedDivision(shape, B, H, H_kv, T, max_len).bytes(d); });
+    return with_form(B, H_kv, H / H_kv * T, d, max_len, cache_dtype == FA_FP8_E4M3,
+                     [&](auto form) { return CachedDivision(form, B, H, H_kv, T, max_len).bytes(d); });
 }
 
 int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
                      void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream) {
     const CachedArgs a = {q, o, cache, counts, tree, lse, nullptr, nullptr, nullptr, B, H, T, tree_batches, 1, 0, scale};
-    return with_shape(H / cache.H_kv * T, d, cache.dtype == FA_FP8_E4M3, [&](auto shape, auto D, auto codes, auto cols, auto rt, auto form) {
-        using Shape = decltype(shape);
-        constexpr int d_ = decltype(D)::value, cols_ = decltype(cols)::value, rt_ = decltype(rt)::value, form_ = decltype(form)::value;
-        constexpr bool codes_ = decltype(codes)::value;
-        return dtype == FA_BF16 ? launch_cached<bf16_tag, Shape, d_, codes_, cols_, rt_, form_>(a, workspace, max_len, stream)
-                                : launch_cached<f16_tag, Shape, d_, codes_, cols_, rt_, form_>(a, workspace, max_len, stream);
+    return with_form(B, cache.H_kv, H / cache.H_kv * T, d, max_len, cache.dtype == FA_FP8_E4M3, [&](auto form) {
+        using Form = decltype(form);
+        return dtype == FA_BF16 ? launch_cached<bf16_tag, Form>(a, workspace, max_len, stream) : launch_cached<f16_tag, Form>(a, workspace, max_len, stream);
     });
 }
 
