@@ -193,6 +193,53 @@ def test_long_caches_are_divided_and_joined(dtype, cache, d, H, H_kv, T, lens):
     assert torch.equal(c.run()[0], o) and torch.equal(c.run()[1], lse)  # repeatable
 
 
+@pytest.mark.parametrize("dtype,cache,d,B,H,H_kv,T,lens", [
+    ("bf16", "bf16", 64, 48, 8, 8, 1, (1, 400)),      # shares that end inside sequences: some teams have two
+    ("f16", "e4m3", 128, 48, 16, 8, 1, (1, 400)),
+    ("bf16", "e4m3", 64, 70, 4, 2, 3, (0, 700)),      # more sequences than a wave has lanes
+    ("f16", "f16", 64, 130, 2, 1, 1, (0, 900)),
+    ("bf16", "bf16", 128, 40, 12, 4, 7, (1, 600)),    # 21 rows
+    ("f16", "e4m3", 64, 24, 12, 4, 16, (1, 500)),     # 48 rows
+    ("bf16", "bf16", 64, 20, 16, 4, 20, (1, 700)),    # 80 rows, one group of them
+    ("bf16", "e4m3", 128, 9, 8, 2, 60, (1, 900)),     # 240 rows, two
+    ("f16", "f16", 256, 7, 4, 2, 70, (1, 600)),       # 140 rows, two
+    ("bf16", "bf16", 256, 30, 32, 4, 2, (1, 500)),
+])
+def test_shares_of_many_sequences(dtype, cache, d, B, H, H_kv, T, lens):
+    g = np.random.default_rng(B + d)
+    lens = g.integers(lens[0], lens[1], B)
+    lens[B // 2] = 0
+    counts = None if T == 1 else g.integers(0, T + 1, B)
+    c = Case(500 + B, dtype, cache, B, H, H_kv, T, d, 16, lens, counts, _random_tree(B, B, T) if T > 1 else None)
+    o, lse = torch.full(c.q.shape, 7.0, dtype=c.q.dtype, device="cuda"), torch.full(c.q.shape[:3], 7.0, device="cuda")
+    for max_len in (1 << 20, 0):  # teams, and whatever the rule says
+        o.fill_(7.0)
+        lse.fill_(7.0)
+        c.run(o=o, lse=lse, max_len=max_len)
+        c.check(o, lse)
+        for b in range(B):
+            assert (o[b, :, c.counts[b]:] == 7).all() and (lse[b, :, c.counts[b]:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype,cache", _KINDS)
+@pytest.mark.parametrize("d,H,H_kv,T", [(64, 8, 2, 40), (128, 2, 2, 9), (128, 16, 4, 12), (256, 8, 2, 20)])
+@pytest.mark.parametrize("max_len", [0, 1 << 20])
+def test_unseen_values_in_every_form(dtype, cache, d, H, H_kv, T, max_len):
+    # values that are not finite in V of new tokens, in 16 to 160 rows, in one launch and joined
+    tree = _random_tree(T, 2, T)
+    c = Case(600 + T, dtype, cache, 2, H, H_kv, T, d, 16, [300, 21], tree=tree)
+    for b in range(2):
+        for u, col, x in ((2, 5, np.nan), (4, d - 1, np.inf), (5, 33, -np.inf), (T - 2, 33, np.inf)):
+            page, slot = cache_oracle.place(c.host, b, int(c.lens[b]) + u)
+            if cache == "e4m3":
+                c.args["v_pages"][page, :, slot, col] = 0x7F
+                c.host["v_pages"][page, :, slot, col] = 0x7F
+            else:
+                c.args["v_pages"][page, :, slot, col] = float(x)
+                c.host["v_pages"][page, :, slot, col] = x
+    c.check(*c.run(max_len=max_len), poison=True)
+
+
 def test_rising_scores_and_large_ones():
     # every key block raises the maximum; scores up to several hundred
     for dtype, cache in _KINDS:
