@@ -15,7 +15,8 @@
  *     inputs, writes outputs, and keeps no reference after the call returns.
  *   - Tensors are contiguous [B, H, N, d] with d fastest (paper section 3.3: inputs are
  *     contiguous in the head dimension); lse / D-like vectors are fp32 [B, H, N].
- *     Every tensor pointer must be 16-byte aligned.
+ *     Every tensor pointer must be 16-byte aligned.  (The calls on rotary positions and on
+ *     a cache take strides too, and say which arrays need less alignment.)
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls are
  *     asynchronous with respect to the host: they enqueue kernels and return.  They
  *     never synchronise, allocate or free device memory, throw, or abort.
@@ -32,7 +33,8 @@
  *     addressed through 32-bit byte offsets, 4*N*d <= 0x7ff00000 (else
  *     FA_ERR_UNSUPPORTED): N <= 4 192 256 at d = 128, twice that at d = 64, half at 256.
  *     HIP refuses a launch of 2^32 threads or more (FA_ERR_LAUNCH): a request of so many short sequences
- *     that its kernel needs them, B*H of 8 million or more, has to be split by the caller.
+ *     that its kernel needs them, B*H of 8 million or more, has to be split by the caller (rotation and
+ *     cache: 2^36 elements or more of a tensor).
  *   - Thread-safe: no mutable global state.
  */
 #ifndef FA_MI355_H
@@ -51,9 +53,9 @@ typedef enum {
     FA_ERR_DTYPE = 3,       /* dtype is not a member of fa_dtype */
     FA_ERR_UNSUPPORTED = 4, /* a valid request this build has no kernel for (e.g. head dim 96) */
     FA_ERR_ALIGN = 5,       /* a tensor pointer is not 16-byte aligned */
-    FA_ERR_WORKSPACE = 6,   /* workspace NULL or smaller than fa_bwd_workspace_bytes() */
+    FA_ERR_WORKSPACE = 6,   /* workspace NULL or smaller than fa_bwd_workspace_bytes() or fa_fwd_cache_workspace_bytes() */
     FA_ERR_LAUNCH = 7,      /* the HIP runtime rejected a launch */
-    FA_ERR_TOO_LARGE = 8    /* fa_bwd_noalloc: B*H*N exceeds FA_BWD_NOALLOC_MAX_ROWS */
+    FA_ERR_TOO_LARGE = 8    /* fa_bwd_noalloc: B*H*N exceeds FA_BWD_NOALLOC_MAX_ROWS; fa_fwd_cache: T exceeds FA_CACHE_MAX_TOKENS */
 } fa_status;
 
 typedef enum {
@@ -270,8 +272,8 @@ int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double 
  *   block_table : int32 [B, max_pages]; token p of sequence b is in slot p % page_size of page block_table[b][p / page_size]
  *   lens        : int32 [B], how many tokens of a sequence the cache holds (less than 0: none)
  * all on the device.  page_size: a multiple of 16 (else FA_ERR_UNSUPPORTED) with 4 page_size d <= 0x7ff00000; a cache that is
- * one contiguous [B, H_kv, max_tokens, d] is one of B pages.  A sequence has max_pages * page_size places (< 2^31).  A page
- * may stand in several sequences' rows of the table.
+ * one contiguous [B, H_kv, max_tokens, d] is one of B pages.  A sequence has max_pages * page_size places, at most
+ * FA_CACHE_MAX_PLACES (else FA_ERR_SHAPE).  A page may stand in several sequences' rows of the table.
  * A table entry outside 0 .. n_pages - 1 is no page: nothing is written to it, and its tokens are neither read back nor seen.
  * The same goes for tokens at or past max_pages * page_size.
  *
@@ -284,6 +286,8 @@ int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double 
  *     scale = a / 448,   code = round-to-nearest-even e4m3 of clamp(x * (448 / a), +-448),   a = max |x| over its finite elements
  * (a = 0: scale 1; 0 < a < 2^-100: a = 2^-100).  So an infinity becomes the largest value of the token, and a NaN stays one.
  */
+#define FA_CACHE_MAX_PLACES 0x7fff0000
+
 int fa_cache_write(const void* k, const long long* k_strides, const void* v, const long long* v_strides,
                    void* k_pages, void* v_pages, float* k_scales, float* v_scales,
                    const int* block_table, const int* lens, const int* counts, int B, int H_kv, int T, int d,
@@ -308,7 +312,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
  *             h / (H / H_kv).
  *   tree    : int32 [tree_batches, T, ceil(T / 32)] (device, read), tree_batches = B, or 1 where all sequences share one
  *   o       : the shape and dtype of q (device, written), strides as in fa_rope; lse : fp32 [B,H,T], contiguous (device, written)
- *             A row that sees nothing gets O = 0 and L = -infinity.  Rows of tokens from counts[b] on stay as they are.
+ *             A row that sees nothing gets O = 0 and L = -infinity.  Rows of tokens from counts[b] on stay as they are.  o and
+ *             lse overlap no other argument.
  *   cache_dtype : dtype, or FA_FP8_E4M3 (another: FA_ERR_UNSUPPORTED)
  *   max_len : what lens[b] + T is expected to reach at most, or 0: max_pages * page_size.  It decides how the keys are
  *             divided over the chip and with that the time, not which of them are seen.  fa_fwd_cache_workspace_bytes takes
@@ -317,8 +322,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
  *             aligned, owned by the caller; calls that may run at the same time need one each.
  * T <= FA_CACHE_MAX_TOKENS (else FA_ERR_TOO_LARGE).  A value or scale in a place that a row does not see, whatever it is,
  * has no influence on the row.  Scores, softmax and the sums are fp32; the probabilities are rounded to the cache's 16-bit
- * type (fp16 with FA_FP8_E4M3) for their product with V.  Nothing is accumulated with atomics: results are bit-for-bit
- * repeatable.
+ * type (fp16 with FA_FP8_E4M3) for their product with V, to two numbers of it with up to 16 rows (H / H_kv * T) to a key/value
+ * head.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One launch, or two where sequences are divided.
  */
 #define FA_CACHE_MAX_TOKENS 256
 

@@ -61,7 +61,7 @@ int check_cache(const fa::Cache& c, int B, int d) {
     if (c.dtype < FA_F32 || c.dtype > FA_FP8_E4M3 || (!codes && (c.k_scales || c.v_scales))) return FA_ERR_DTYPE;
     if (c.dtype == FA_F32) return FA_ERR_UNSUPPORTED;
     if (B <= 0 || c.H_kv <= 0 || d <= 0 || c.page_size <= 0 || c.n_pages <= 0 || c.max_pages <= 0) return FA_ERR_SHAPE;
-    if ((long)c.max_pages * c.page_size > 0x7fffffffL) return FA_ERR_SHAPE;
+    if ((long)c.max_pages * c.page_size > FA_CACHE_MAX_PLACES) return FA_ERR_SHAPE;
     if (!head_dim_ok(d) || c.page_size % 16 != 0 || (long)c.page_size * d * 4 > 0x7ff00000L) return FA_ERR_UNSUPPORTED;
     if (!aligned16(c.k) || !aligned16(c.v) || !aligned_to(c.k_scales, 4) || !aligned_to(c.v_scales, 4) ||
         !aligned_to(c.block_table, 4) || !aligned_to(c.lens, 4))

@@ -651,7 +651,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 float top = 0.f;  // the largest finite scale of V in the tile
 #pragma unroll
                 for (int r = 0; r < NS; ++r) top = fmaxf(top, vscale[r] < INFINITY ? vscale[r] : 0.f);
-                top = fminf(fmaxf(M::max_parts(top), 0x1p-100f), 0x1p126f);
+                top = fminf(fmaxf(M::max_parts(top), 0x1p-126f), 0x1p126f);  // (F and 1 / F are normal numbers)
                 const float new_F = __builtin_bit_cast(float, (int)((__builtin_bit_cast(int, top) + 0x7fffff) & 0x7f800000));
                 if (__builtin_amdgcn_readfirstlane(new_F > F)) {
                     const float down = F / new_F;
