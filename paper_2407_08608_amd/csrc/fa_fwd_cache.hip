@@ -46,6 +46,11 @@ struct CachedArgs {
 
 namespace {
 
+// Operands from the LDS go to the matrix instructions this many reads at a time, all issued before the first product: left to itself
+// the compiler has one or two on the way, and each instruction of 16 or 32 cycles waits for one.  us before / after: 4 trees of 32, 4 heads
+// of d = 256 to a key/value head 47.8 / 42.8; 8 trees of 32, 8 heads, codes 53.8 / 51.2; 2 long sequences of codes, d = 256 35.3 / 33.9;
+// within the noise where a CU has 8 waves of 32 columns on 16-bit keys.  4, 8 and 16 are alike.
+constexpr int kReadsAhead = 8;
 constexpr float kLazy = 8.0f;  // the reference of a row rises when a tile's maximum exceeds it by more (log2 units)
 
 // What a sequence has: places before the new tokens, new tokens, all keys
@@ -596,11 +601,18 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 for (int x = 0; x < RT; ++x)
 #pragma unroll
                     for (int kt = 0; kt < M::TILES; ++kt) y[x][kt] = typename M::Acc{};
-                static_for<Tile::KR>([&](auto n) __attribute__((always_inline)) {
-                    constexpr int k = decltype(n)::value;
-                    static_for<M::TILES>([&](auto m) __attribute__((always_inline)) {
-                        constexpr int kt = decltype(m)::value;
-                        const i32x4 w = at.template row_read<k, kt>(kK);
+                constexpr int READS = Tile::KR * M::TILES, AT_ONCE = READS < kReadsAhead ? READS : kReadsAhead;
+                static_for<READS / AT_ONCE>([&](auto n) __attribute__((always_inline)) {
+                    constexpr int first = decltype(n)::value * AT_ONCE;
+                    i32x4 read[AT_ONCE];
+                    static_for<AT_ONCE>([&](auto m) __attribute__((always_inline)) {
+                        constexpr int j = first + decltype(m)::value;
+                        read[j - first] = at.template row_read<j / M::TILES, j % M::TILES>(kK);
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                    static_for<AT_ONCE>([&](auto m) __attribute__((always_inline)) {
+                        constexpr int j = first + decltype(m)::value, k = j / M::TILES, kt = j % M::TILES;
+                        const i32x4 w = read[j - first];
                         if constexpr (CODES) {
                             const i32x4 lo = from_codes<Tag>(w[0], w[1]), hi = from_codes<Tag>(w[2], w[3]);
 #pragma unroll
@@ -672,6 +684,29 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                 for (int r = 0; r < NS; ++r) vscale[r] *= inv_F;
             }
+            auto see_to_odd_ones = [&]() __attribute__((always_inline)) {
+                if (special && key + 32 > ext.len)
+                    if (__builtin_expect(at.not_finite(kV, lane), 0)) {
+                        odd = 1;
+                        if constexpr (SHARED) barrier();  // all waves have seen it; then each clears all
+                        at.clear_not_finite(kV, lane);
+                    }
+            };
+            constexpr int COLUMN_READS = M::SLABS * NT, COLUMNS_AT_ONCE = COLUMN_READS < kReadsAhead ? COLUMN_READS : kReadsAhead;
+            i32x4 columns[COLUMNS_AT_ONCE];
+            auto read_columns = [&](auto n) __attribute__((always_inline)) {
+                constexpr int first = decltype(n)::value * COLUMNS_AT_ONCE;
+                static_for<COLUMNS_AT_ONCE>([&](auto m) __attribute__((always_inline)) {
+                    constexpr int j = first + decltype(m)::value;
+                    columns[j - first] = at.template columns<j % NT, j / NT>(kV);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            if constexpr (SHARED) {  // (V is there: its first operands arrive beside the softmax)
+                before_products();
+                see_to_odd_ones();
+                read_columns(std::integral_constant<int, 0>{});
+            }
             i32x4 pb[RT][M::SLABS], rest[RT][M::SLABS];  // what V is multiplied by
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
@@ -714,18 +749,18 @@ fa_fwd_cache_kernel(CachedArgs a) {
                             PE::pack2(s[x][r] - PE::to_float((uint16_t)w), s[x][r + 1] - PE::to_float((uint16_t)((uint32_t)w >> 16)));
                 }
             }
-            before_products();
-            if (special && key + 32 > ext.len)
-                if (__builtin_expect(at.not_finite(kV, lane), 0)) {
-                    odd = 1;
-                    if constexpr (SHARED) barrier();  // all waves have seen it; then each clears all
-                    at.clear_not_finite(kV, lane);
-                }
+            if constexpr (!SHARED) {
+                before_products();
+                see_to_odd_ones();
+                read_columns(std::integral_constant<int, 0>{});
+            }
             // O^T += V^T P^T
-            static_for<M::SLABS>([&](auto sl) __attribute__((always_inline)) {
-                static_for<NT>([&](auto d) __attribute__((always_inline)) {
-                    constexpr int slab = decltype(sl)::value, dt = decltype(d)::value;
-                    i32x4 w = at.template columns<dt, slab>(kV);
+            static_for<COLUMN_READS / COLUMNS_AT_ONCE>([&](auto n) __attribute__((always_inline)) {
+                constexpr int first = decltype(n)::value * COLUMNS_AT_ONCE;
+                if constexpr (first > 0) read_columns(n);
+                static_for<COLUMNS_AT_ONCE>([&](auto m) __attribute__((always_inline)) {
+                    constexpr int j = first + decltype(m)::value, slab = j / NT, dt = j % NT;
+                    i32x4 w = columns[j - first];
                     if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
 #pragma unroll
                     for (int x = 0; x < RT; ++x) {
