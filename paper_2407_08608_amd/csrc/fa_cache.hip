@@ -3,7 +3,7 @@
 //
 // Every element is read once and written once, and nothing is computed that takes longer: HBM decides, for a token of each
 // sequence the launch.  Measured at d = 128: 138 MB written as codes in 29 us (4.7 TB/s), 142 MB read back from codes in 29 us
-// (4.9 TB/s; a copy reaches 5.0).  A row (a token of one head) is d / 16 lanes of 16 elements, its K and its V in the same lanes, so twice
+// (4.8 TB/s; a copy reaches 5.0).  A row (a token of one head) is d / 16 lanes of 16 elements, its K and its V in the same lanes, so twice
 // the bytes are in flight; the largest magnitude of a row is found across its lanes by DPP, without the LDS.
 #include "fa_device.h"
 #include "fa_launch.h"

@@ -8,8 +8,8 @@
 // The floor is HBM's up to some 250 rows to a key/value head (4 rows d flops for 4 d bytes of a 16-bit key, at 1.2 PFLOP/s of a
 // library product and 5 TB/s of a copy): the cache is read once per row group, straight into the LDS.  Measured with the join:
 // 32 sequences of 500 to 4096 keys, H = 32 on 8, bf16, T = 1: 268 MB in 51 us, 5.2 TB/s; 2 of up to 65536 keys, H = 16 on 2,
-// d = 256, codes: 129 MB in 34 us, of which 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
-// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 92 us, where the matrix pipes are busy a third of the loop.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// d = 256, codes: 129 MB in 33 us, of which some 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
+// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 90 us, where the matrix pipes are busy a third of the loop.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
 // refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
