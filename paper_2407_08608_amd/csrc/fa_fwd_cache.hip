@@ -21,8 +21,8 @@
 //   - Masks: only tiles that reach the new tokens (or hold a bad page) look at one.  What a lane's row sees of a tile is a 32-bit
 //     word: places before the new tokens, the row's window of the tree, the tokens that are there.
 //   - e4m3: codes become 16-bit operands in registers (exact): K in the type of Q, with the key's scale on the score; V in
-//     fp16, with P~ = p (v scale / F), F a power of two not below the scales so far.  So P~ is at most 2^kLazy in fp16 whatever
-//     the scales are, and eleven bits of each weight reach the product.
+//     bf16, with P~ = p v scale as two bf16 numbers, a rounded value and what that leaves out.  Their range is that of the scales, so
+//     no weight depends on a scale of another key, seen or not, and sixteen bits of each reach the product.
 //   - 16 columns where a group has no more rows (v_mfma_16x16x32 instead of 32x32x16): half the registers, matrix and vector
 //     instructions for a tile.
 #include "fa_device.h"
@@ -173,7 +173,7 @@ static __device__ __forceinline__ void once_to_lds_16B(const BufferWords& rsrc, 
 template <typename Tag, int D, bool CODES, int COLS>
 struct CacheTile {
     using M = Matrix<Tag, D, COLS>;
-    using PE = std::conditional_t<CODES, f16_tag, Tag>;  // of the product with V
+    using PE = std::conditional_t<CODES, bf16_tag, Tag>;  // of the product with V
     using PM = Matrix<PE, D, COLS>;
     static constexpr int ROWB = D * (CODES ? 1 : 2), TILE_B = 32 * ROWB, CPR = ROWB / 16, RPI = 1024 / ROWB, NI = 32 / RPI;
     static constexpr int MASK = CPR < 16 ? CPR - 1 : 15;
@@ -342,7 +342,7 @@ struct CachedShape {
     static constexpr int SCALE_B = CODES ? 256 : 0;             // of a tile: 32 scales of K, 32 of V
     static constexpr int STAGE_B = 2 * Tile::TILE_B + SCALE_B, STAGES_B = STG * STAGE_B * (SHARED ? 1 : NW);
     static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
-    static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 3 * 4 + NW * 4;
+    static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 2 * 4 + NW * 4;
     static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
     // workgroups (of four waves) to a CU, by registers
     static constexpr int WAVES = SHARED ? (D == 64 ? 3 : D == 128 ? 2 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
@@ -364,7 +364,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
     constexpr bool ACCUMULATION = Shape::WAVES == 1;  // more than 256 registers: accumulators in the half for matrix results
     // Few rows leave the matrix pipes idle: P goes in as its rounded value and what that leaves out, so that its rounding does not
     // add to the output's (error against 64 bits, bf16, of the output's rounding alone: 1.4 times / 1.0 times; the time is the same)
-    constexpr bool TWO_PARTS = COLS == 16;
+    // With codes always: one bf16 number would be eight times as coarse as the fp16 number that a factor common to all keys allows, and
+    // no common factor is right where a key of a large scale weighs little, or nothing (8 trees of 32 tokens, 8 heads: 53.0 us, with
+    // fp16 and such a factor 51.3; 64 x 500 to 4096 keys, T = 1, d = 64: 26.1 and 27.8).
+    constexpr bool TWO_PARTS = COLS == 16 || CODES;
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -563,7 +566,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
 
     typename M::Acc acc[RT][NT];
     float m_run[RT], l_run[RT];
-    float F = 0.f, inv_F = 0.f;  // codes: the power of two that P~ is divided by
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         m_run[x] = -INFINITY;
@@ -658,31 +660,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                     for (int r = 0; r < NS; ++r) s[x][r] = seen[x] >> M::bit(r) & 1 ? s[x][r] : -INFINITY;
                 }
-                if constexpr (CODES)
-#pragma unroll
-                    for (int r = 0; r < NS; ++r) vscale[r] = live >> (part << M::SHIFT) >> M::bit(r) & 1 ? vscale[r] : 0.f;
-            }
-            if constexpr (CODES) {
-                float top = 0.f;  // the largest finite scale of V in the tile
-#pragma unroll
-                for (int r = 0; r < NS; ++r) top = fmaxf(top, vscale[r] < INFINITY ? vscale[r] : 0.f);
-                top = fminf(fmaxf(M::max_parts(top), 0x1p-126f), 0x1p126f);  // (F and 1 / F are normal numbers)
-                const float new_F = __builtin_bit_cast(float, (int)((__builtin_bit_cast(int, top) + 0x7fffff) & 0x7f800000));
-                if (__builtin_amdgcn_readfirstlane(new_F > F)) {
-                    const float down = F / new_F;
-                    F = new_F;
-                    inv_F = 1.f / new_F;
-#pragma unroll
-                    for (int x = 0; x < RT; ++x)
-#pragma unroll
-                        for (int dt = 0; dt < NT; ++dt) {
-                            if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));
-                            acc[x][dt] *= down;
-                            if constexpr (ACCUMULATION) asm volatile("" : "+a"(acc[x][dt]));
-                        }
-                }
-#pragma unroll
-                for (int r = 0; r < NS; ++r) vscale[r] *= inv_F;
             }
             auto see_to_odd_ones = [&]() __attribute__((always_inline)) {
                 if (special && key + 32 > ext.len)
@@ -736,7 +713,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                     if constexpr (CODES) s[x][r] = p * vscale[r];
                 }
                 if constexpr (CODES)
-                    if (special)  // a scale that is not finite belongs to those rows only that see it
+                    if (special)  // (of a place that a row does not see P is 0, but its scale need not be finite)
 #pragma unroll
                         for (int r = 0; r < NS; ++r) s[x][r] = seen[x] >> M::bit(r) & 1 ? s[x][r] : 0.f;
                 l_run[x] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
@@ -761,7 +738,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 static_for<COLUMNS_AT_ONCE>([&](auto m) __attribute__((always_inline)) {
                     constexpr int j = first + decltype(m)::value, slab = j / NT, dt = j % NT;
                     i32x4 w = columns[j - first];
-                    if constexpr (CODES) w = from_codes<f16_tag>(w[0], w[1]);
+                    if constexpr (CODES) w = from_codes<bf16_tag>(w[0], w[1]);
 #pragma unroll
                     for (int x = 0; x < RT; ++x) {
                         acc[x][dt] = PM::mma(w, pb[x][slab], acc[x][dt]);
@@ -806,19 +783,18 @@ fa_fwd_cache_kernel(CachedArgs a) {
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last requests: the LDS is about to be reused
 
-    // The states of waves that divided the keys meet: with M the largest reference and f = 2^(m - M), sum f F acc, M and sum f l
-    float* const state = reinterpret_cast<float*>(lds + Shape::LDS - Shape::STATE_B);  // [RT][NW][COLS][m, l, F]
-    int* const odd_waves = reinterpret_cast<int*>(state + NW * COLS * RT * 3);
+    // The states of waves that divided the keys meet: with M the largest reference and f = 2^(m - M), sum f acc, M and sum f l
+    float* const state = reinterpret_cast<float*>(lds + Shape::LDS - Shape::STATE_B);  // [RT][NW][COLS][m, l]
+    int* const odd_waves = reinterpret_cast<int*>(state + NW * COLS * RT * 2);
     if (lane == 0) odd_waves[wave] = odd;
     float* const merge = reinterpret_cast<float*>(lds);                                // [NW][COLS][MERGE_STRIDE]
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const float l = M::sum_parts(l_run[x]);
         if (part == 0) {
-            float* at = state + ((x * NW + wave) * COLS + col) * 3;
+            float* at = state + ((x * NW + wave) * COLS + col) * 2;
             at[0] = m_run[x] * sc;
             at[1] = l;
-            at[2] = CODES ? F : 1.f;
         }
     }
     constexpr int MC = Shape::MERGE_COLS, MS = Shape::MERGE_STRIDE;
@@ -842,14 +818,13 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 const int g = row / per, tok = row - g * per;
                 float m_all = -INFINITY, l_all = 0.f, f[KW];
 #pragma unroll
-                for (int w = 0; w < KW; ++w) m_all = fmaxf(m_all, state[((x * NW + rw + w) * COLS + r) * 3]);
+                for (int w = 0; w < KW; ++w) m_all = fmaxf(m_all, state[((x * NW + rw + w) * COLS + r) * 2]);
                 const float m_ref = m_all == -INFINITY ? 0.f : m_all;
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
-                    const float* at = state + ((x * NW + rw + w) * COLS + r) * 3;
+                    const float* at = state + ((x * NW + rw + w) * COLS + r) * 2;
                     f[w] = fast_exp2(at[0] - m_ref);
                     l_all += f[w] * at[1];
-                    f[w] *= at[2];
                 }
                 float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
