@@ -265,8 +265,8 @@ struct CacheTile {
     }
 
     // An infinity or a NaN in V of a new token is no business of the rows that do not see it, and a product with P = 0 would
-    // make it theirs.  So where a tile has one (not_finite) it is a zero for the product (clear_not_finite), and the rows that see it
-    // get it at the end.
+    // make it theirs.  So where a tile with new tokens has one (not_finite) it is a zero for the product (clear_not_finite), one of an
+    // old token in the tile too, and the rows that see it get it at the end.
     static constexpr int EXPONENT = CODES ? 0x7F7F7F7F : std::is_same_v<Tag, bf16_tag> ? 0x7F807F80 : 0x7C007C00;
     // the elements of a word that are not finite, all bits of each
     static __device__ __forceinline__ uint32_t odd_ones(uint32_t w) {
@@ -591,7 +591,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
         return vis & live;
     };
 
-    int odd = 0;  // whether V of a new token held a value that is not finite
+    int odd = 0;  // whether V of a tile with new tokens held a value that is not finite
     // A tile: scores, softmax, products.  `at`: where it is (K, V, scales from OFFSET on); `bad`: the halves that are on no page
     auto work = [&](const Tile& at, auto off, int key, int bad, auto&& after_scores, auto&& before_products, auto&& after_products) __attribute__((always_inline)) {
             constexpr int kK = decltype(off)::value, kV = kK + Tile::TILE_B, kScales = kK + 2 * Tile::TILE_B;
@@ -839,9 +839,9 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                 for (int w = 0; w < KW; ++w) any_odd |= odd_waves[rw + w];
                 if (__builtin_expect(any_odd != 0, 0))
-                    for (int u = max(key0 - ext.len, 0); u < key1 - ext.len; ++u) {  // new tokens of these keys that the row sees
-                        const int place = ext.len + u, entry = place / a.c.page_size, words = (a.T + 31) >> 5;
-                        const bool sees = a.tree ? a.tree[((long)(a.tree_batches == 1 ? 0 : b) * a.T + tok) * words + (u >> 5)] >> (u & 31) & 1 : u <= tok;
+                    for (int place = max(key0, ext.len & ~31); place < key1; ++place) {  // from the first tile with a new token on
+                        const int u = place - ext.len, entry = place / a.c.page_size, words = (a.T + 31) >> 5;
+                        const bool sees = u < 0 ? true : a.tree ? a.tree[((long)(a.tree_batches == 1 ? 0 : b) * a.T + tok) * words + (u >> 5)] >> (u & 31) & 1 : u <= tok;
                         const int page = a.c.block_table[(long)b * a.c.max_pages + entry];
                         if (!sees || page < 0 || page >= a.c.n_pages) continue;
                         const long at = (((long)page * H_kv + kvh) * a.c.page_size + (place - entry * a.c.page_size)) * D + c0 + cc;

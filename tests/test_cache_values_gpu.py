@@ -123,3 +123,32 @@ def test_scales_of_either_sign(dtype, d, H, H_kv, T):
             c.host[x], c.args[x] = s, torch.from_numpy(s).cuda()
         for max_len in (0, 1 << 20):
             _check(c, *c.run(max_len=max_len))
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("d,H,H_kv,T", [(64, 8, 4, 1), (128, 16, 2, 1), (256, 4, 1, 1)] + _FORMS)
+@pytest.mark.parametrize("max_len", [0, 1 << 20])
+def test_values_of_old_tokens_that_are_not_finite(dtype, cache, d, H, H_kv, T, max_len):
+    # every row sees them: beside the new tokens in their tile of 32 keys (100 is 96 + 4), and far from them
+    B, n = 2, 100
+    c = Case(970 + T, dtype, cache, B, H, H_kv, T, d, 16, [n, n - 3], tree=_random_tree(T, B, T) if T > 1 else None)
+    for b, p, col, x in ((0, 96, 3, np.nan), (0, 99, 17, np.inf), (1, 96, 40, -np.inf), (1, 5, 41, np.nan), (1, 40, 42, np.inf)):
+        page, slot = cache_oracle.place(c.host, b, p)
+        x = 0x7F if cache == "e4m3" else float(x)
+        c.args["v_pages"][page, :, slot, col] = x
+        c.host["v_pages"][page, :, slot, col] = x
+    o, lse = c.run(max_len=max_len)
+    o64 = f64(o)
+    bad = [(0, 3), (0, 17), (1, 40), (1, 41), (1, 42)]
+    for b, col in bad:
+        assert not np.isfinite(o64[b, :, :, col]).any(), (b, col)
+        if cache != "e4m3" and col in (17, 40):
+            assert (o64[b, :, :, col] == (np.inf if col == 17 else -np.inf)).all()
+    # the other columns as with zeros there
+    fine = [i for i in range(d) if i not in {col for _, col in bad}]
+    clean = dict(c.args, v_pages=c.args["v_pages"].clone())
+    for b, p, col in ((0, 96, 3), (0, 99, 17), (1, 96, 40), (1, 5, 41), (1, 40, 42)):
+        page, slot = cache_oracle.place(c.host, b, p)
+        clean["v_pages"][page, :, slot, col] = 0
+    want = c.run(max_len=max_len, **clean)
+    assert torch.equal(o[..., fine], want[0][..., fine]) and torch.equal(lse, want[1])
