@@ -14,7 +14,7 @@
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
 //     has of such a one, (sum p v, reference, sum p), goes to the workspace, and a second launch joins it with what the teams
-//     before and after have, in that order.  Where there is nothing to even out a workgroup has a whole sequence and head.
+//     before and after have, in that order.  Where no sequence can be long a workgroup has a whole one of a head (whole_sequences).
 //   - Pages: 16 consecutive places lie in one page (page_size is a multiple of 16), so a tile has two resources.  Lane i of a
 //     wave looks up the two rows of the wave's i-th tile, 64 tiles at a time; what is no page, or past the last key, gets a
 //     resource of length 0 and arrives as zeros.
@@ -963,20 +963,30 @@ __global__ void __launch_bounds__(256) fa_join_kernel(CachedArgs a, int ways) {
 }
 
 // Whether each workgroup has a whole sequence and head: one launch, and nothing is looked for or joined, but the longest sequence
-// decides.  So up to a length that goes with the workgroups there are (where they fill the chip anyway, any), in keys that take as
-// long as those of 16 rows at d = 128.  us, whole / teams, by workgroups and the longest of lengths spread over its last third
+// decides.  So up to a length that goes with the workgroups there are, in keys that take as long as those of 16 rows at d = 128, and
+// where they fill the chip up to kAlone keys, whatever these take: there the second start of a team costs more than even shares
+// give, until a sequence much longer than the others keeps its workgroups busy when all others are done.  us, whole / teams, by workgroups and the longest of lengths spread over its last third
 // (T = 1) or half, bf16:
 //   T = 1 d = 64   8: 768 8.9 / 10.5, 1536 12.7 / 10.9;  128: 1536 15.0 / 15.3;  256: 3000 29.5 / 34.2;  512: 4500 79 / 84
 //         d = 128  8: 512 9.5 / 11.4, 1024 13.1 / 11.7;  128: 1024 16.1 / 17.5;  256: 3000 55 / 59, but spread from a tenth of it on
 //                  4096 55.6 / 51.5;  512: 4500 155 / 160
 //   32 rows        32: 1024 16.0 / 16.7;  128: 2048 28 / 29;  256: 4500 77 / 84.   64 rows  64: 768 21.0 / 20.8;  128: 2048 35 / 38
 //   256 rows       128: 512 25.9 / 28.3, 768 32 / 30;  256: 1024 41 / 46, 2048 66 / 59;  512: 4500 157 / 166
+// and where they fill the chip, lengths alike (the last third) | one so long, the others 500 to 2000 (64 or 32 sequences of 8 heads):
+//   T = 1 d = 64   512: 4500 79 / 83, 9000 148 / 149, 16000 264 / 266 | 4500 42 / 37, 9000 70 / 35, 65536 400 / 58
+//         d = 128  512: 4500 153 / 160, 9000 296 / 294, 16000 528 / 521 | 4500 75 / 66, 9000 120 / 60, 65536 608 / 104
+//         d = 256  512: 4500 305 / 313, 9000 587 / 576 | 4500 132 / 128, 9000 201 / 121, 65536 1174 / 202
+//         codes, d = 128  512: 4500 83 / 88, 9000 154 / 156 | 4500 47 / 39, 9000 80 / 37, 65536 476 / 65
+//   32 rows, d = 128   256: 4500 81 / 95, 9000 159 / 168 | 4500 57 / 45, 9000 95 / 48, 32768 306 / 72
+//   64 rows, d = 128   256: 4500 86 / 109, 9000 163 / 183 | 4500 62 / 61, 9000 101 / 64
+//   256 rows, d = 128  512: 4500 170 / 185, 9000 318 / 325 | 4500 123 / 95, 9000 220 / 100
+constexpr int kAlone = 4608;
 template <typename Form>
 static bool whole_sequences(double workgroups, int max_len) {
     constexpr bool shared = Form::FORM == kShareKeys;
     constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
                      d256 = Form::COLS == 16 ? (Form::CODES ? 1.5 : 2.0) : shared ? 2.0 : 1.25;
-    if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return true;
+    if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return max_len <= kAlone;
     const double limit = 8 * workgroups + 256 > 512 ? 8 * workgroups + 256 : 512;
     return max_len * (Form::D == 64 ? d64 : Form::D == 128 ? d128 : d256) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
 }
