@@ -472,9 +472,9 @@ def fa_cache_read(k_pages, v_pages, block_table, lens, N=None, dtype=None, k_sca
 
 
 def fa_tree_words(visible):
-    """The `tree` of fa_fwd_cache, int32 [..., T, ceil(T / 32)], from visible[..., t, u]: whether new token t sees new token u."""
+    """The `tree` of fa_fwd_cache, int32 [..., T, ceil(T / 32)], from visible[..., t, u]: whether (not zero) new token t sees new token u."""
     T = visible.shape[-1]
-    bits = torch.nn.functional.pad(visible.to(torch.int64), (0, -T % 32)).unflatten(-1, (-1, 32))
+    bits = torch.nn.functional.pad((visible != 0).to(torch.int64), (0, -T % 32)).unflatten(-1, (-1, 32))
     words = (bits << torch.arange(32, device=visible.device)).sum(-1)
     return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
 
