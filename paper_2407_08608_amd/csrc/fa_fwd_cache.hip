@@ -9,7 +9,7 @@
 // library product and 5 TB/s of a copy): the cache is read once per row group, straight into the LDS.  Measured with the join:
 // 32 sequences of 500 to 4096 keys, H = 32 on 8, bf16, T = 1: 268 MB in 51 us, 5.2 TB/s; 2 of up to 65536 keys, H = 16 on 2,
 // d = 256, codes: 129 MB in 33 us, of which some 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
-// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 90 us, where the matrix pipes are busy a third of the loop.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
 // refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
@@ -49,7 +49,7 @@ namespace {
 // Operands from the LDS go to the matrix instructions this many reads at a time, all issued before the first product: left to itself
 // the compiler has one or two on the way, and each instruction of 16 or 32 cycles waits for one.  us before / after: 4 trees of 32, 4 heads
 // of d = 256 to a key/value head 47.8 / 42.8; 8 trees of 32, 8 heads, codes 53.8 / 51.2; 2 long sequences of codes, d = 256 35.3 / 33.9;
-// within the noise where a CU has 8 waves of 32 columns on 16-bit keys.  4, 8 and 16 are alike.
+// within the noise where a CU has 8 waves of 32 columns on 16-bit keys.  4, 8 and 16 are alike.  (Codes: with each weight in one fp16 number.)
 constexpr int kReadsAhead = 8;
 constexpr float kLazy = 8.0f;  // the reference of a row rises when a tile's maximum exceeds it by more (log2 units)
 
@@ -158,7 +158,8 @@ template <typename Tag, int D> struct Matrix<Tag, D, 16> {
     }
 };
 
-// global_to_lds_16B of what nobody else reads
+// global_to_lds_16B, non-temporal: what nobody else reads.  (But at d = 256 two row groups of 33 to 64 rows read each key, through this
+// too: no form there takes more than 32 rows a workgroup and divides the keys.)
 static __device__ __forceinline__ void once_to_lds_16B(const BufferWords& rsrc, uint32_t lds_base, int byte_off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
                  :
@@ -995,8 +996,8 @@ static bool whole_sequences(double workgroups, int max_len) {
 //   rows to a key/value head  up to 16: 16 columns; 17 to 32: 32; 33 to 64: two tiles of 32 to a wave, so that each operand is read once for
 //   both; more: four tiles, a wave each, that share what is staged (256 rows 94 us, divided keys 115; 52 rows 27.4 and 25.9).
 // Eight waves instead of four halve the chain of a sequence that a workgroup has for itself, where its keys are small enough for two
-// such workgroups' worth of LDS to be worth it: us, four / eight, T = 1, 8 heads: d = 64 1024 10.1 / 8.6; codes d = 128 768 13.0 / 10.6,
-// d = 256 512 15.7 / 13.7; bf16 d = 128 768 11.2 / 10.3 but 2048 22.2 / 21.7, and 300 7.5 / 7.7.
+// such workgroups' worth of LDS to be worth it: us, four / eight, T = 1, 8 heads: d = 64 1024 9.7 / 8.3; codes d = 64 768 9.9 / 8.1,
+// d = 128 768 10.5 / 9.3, d = 256 512 12.7 / 11.6; bf16 d = 128 768 11.2 / 10.3 but 2048 22.2 / 21.7, and 300 7.5 / 7.7.
 template <int D_, bool CODES_, int COLS_, int RT_, int NW_, int FORM_>
 struct CachedForm {
     static constexpr int D = D_, COLS = COLS_, RT = RT_, NW = NW_, FORM = FORM_, STG = FORM == kShareKeys ? 3 : 1;

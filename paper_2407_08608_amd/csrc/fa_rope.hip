@@ -127,9 +127,10 @@ __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
 }
 
 // Whether the inputs are read past the caches: so many bytes do not stay there until they are read anyway, and push the outputs out,
-// which the next call reads.  us, kept / past, MiB of input; after other inputs | after a launch that writes them (included):
-//   8 5.9 / 5.9 | 13.5 / 13.6;  32 12.2 / 13.7 | 26.6 / 26.3;  64 24.7 / 24.9 | 41.5 / 39.8;  80 33.5 / 30.0 | 48.2 / 46.7;
-//   109 46.9 / 39.0 | 61.0 / 59.6;  128 55.1 / 44.8 | 68.7 / 73.3;  188 78.0 / 78.8 | 106 / 96.5;  256 99.9 / 99.9 | 161 / 133
+// which the next call reads.  us, kept / past, MiB of input (bf16, 16 and 16 heads of 128, a projection's layout); after other inputs |
+// after a launch that writes them (included):
+//   32 16.0 / 17.7 | 26.5 / 26.7;  64 28.1 / 28.2 | 47.0 / 46.2;  80 34.9 / 33.0 | 62.5 / 57.0;  96 44.5 / 39.4 | 80.3 / 69.7;
+//   109 50.0 / 41.6 | 90.0 / 78.4;  128 55.6 / 48.1 | 105 / 98;  150 68.2 / 63.6 | 120 / 114;  188 82.4 / 80.9 | 144 / 139;  256 116 / 112 | 199 / 196
 constexpr double kReadOnce = 72.0 * 1024 * 1024;
 
 template <int D, int DTYPE>
