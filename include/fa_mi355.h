@@ -317,17 +317,17 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
  *   cache_dtype : dtype, or FA_FP8_E4M3 (another: FA_ERR_UNSUPPORTED)
  *   max_len : what lens[b] + T is expected to reach at most, or 0: max_pages * page_size.  It decides how the keys are
  *             divided over the chip and with that the time (far too large a number costs up to 1.7 times where all sequences are
- *             short), not which of them are seen.  fa_fwd_cache_workspace_bytes takes
- *             the same number, and max_pages * page_size in place of 0.
+ *             short), not which of them are seen.  fa_fwd_cache_workspace_bytes takes the same number, and max_pages * page_size
+ *             in place of 0.
  *   workspace : device scratch of at least fa_fwd_cache_workspace_bytes(...) bytes (which can be 0: then it may be NULL), 16-byte
  *             aligned, owned by the caller; calls that may run at the same time need one each.
  * T <= FA_CACHE_MAX_TOKENS (else FA_ERR_TOO_LARGE).  A value or scale in a place that a row does not see, whatever it is,
  * has no influence on the row; an infinity or NaN in V that it sees makes its element of O one or the other.  Scores, softmax and
  * the sums are fp32.  For their product with V the probabilities are rounded to the 16-bit type of the cache, to two numbers of it
  * (a value and what that leaves out) with up to 16 rows (H / H_kv * T) to a key/value head; with FA_FP8_E4M3 the probabilities
- * times V's scales, which may have either sign, to two bf16 numbers always.  sum p |v|, where the largest p of a row is at most 2^8,
- * has to stay within fp32.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One launch, or two where
- * sequences are divided.
+ * times V's scales, which may have either sign, to two bf16 numbers always.  With p up to 2^8 for the largest of a row, sum p |v| and
+ * p times V's scales have to stay within fp32.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One
+ * launch, or two where sequences are divided.
  */
 #define FA_CACHE_MAX_TOKENS 256
 
