@@ -53,7 +53,7 @@ typedef enum {
     FA_ERR_DTYPE = 3,       /* dtype is not a member of fa_dtype */
     FA_ERR_UNSUPPORTED = 4, /* a valid request this build has no kernel for (e.g. head dim 96) */
     FA_ERR_ALIGN = 5,       /* a tensor pointer is not 16-byte aligned */
-    FA_ERR_WORKSPACE = 6,   /* workspace NULL or smaller than fa_bwd_workspace_bytes() or fa_fwd_cache_workspace_bytes() */
+    FA_ERR_WORKSPACE = 6,   /* workspace NULL or smaller than the call's *_workspace_bytes() */
     FA_ERR_LAUNCH = 7,      /* the HIP runtime rejected a launch */
     FA_ERR_TOO_LARGE = 8    /* fa_bwd_noalloc: B*H*N exceeds FA_BWD_NOALLOC_MAX_ROWS; fa_fwd_cache: T exceeds FA_CACHE_MAX_TOKENS */
 } fa_status;
@@ -62,7 +62,8 @@ typedef enum {
     FA_F32 = 0,     /* fp32 in / fp32 out, fp32 arithmetic (d = 64 only) */
     FA_BF16 = 1,    /* bf16 in / bf16 out, fp32 accumulate */
     FA_F16 = 2,     /* fp16 in / fp16 out, fp32 accumulate */
-    FA_FP8_E4M3 = 3 /* OCP e4m3 ("fn") codes in, bf16 out, fp32 accumulate */
+    FA_FP8_E4M3 = 3, /* OCP e4m3 ("fn") codes in, bf16 out, fp32 accumulate */
+    FA_FP4_E2M1 = 4  /* OCP e2m1 codes over a power of two for each 32 elements: of a cache only (elsewhere FA_ERR_DTYPE) */
 } fa_dtype;
 
 /*
@@ -248,6 +249,26 @@ int fa_rope_bwd(const void* dq, const long long* dq_strides, const void* dk, con
                 float amplitude, int interleaved, int dtype, void* stream);
 
 /*
+ * Rotary positions with several axes: the frames, rows and columns of images and video next to the places of text.  As fa_rope and
+ * fa_rope_bwd, but pair i goes by an axis of its own,
+ *     phi_i = positions[axis[i]][b][n] * inv_freq[i]
+ * so that any share of the pairs, in one run or dealt in turn, can go to each axis.
+ *   axis     : int32 [rot_dim / 2] (device, read); a pair whose axis is not in 0 .. axes - 1 is not turned (phi = 0; A applies)
+ *   positions: int32 [axes, B, N], any value (device, read)
+ *   axes     : at least 1 (else FA_ERR_SHAPE)
+ * axis and positions may not be NULL.  Everything else as documented for fa_rope.
+ */
+int fa_rope_axes(const void* q, const long long* q_strides, const void* k, const long long* k_strides,
+                 void* q_out, const long long* q_out_strides, void* k_out, const long long* k_out_strides,
+                 const double* inv_freq, const int* axis, const int* positions, int axes, int B, int H, int H_kv, int N, int d,
+                 int rot_dim, float amplitude, int interleaved, int dtype, void* stream);
+
+int fa_rope_axes_bwd(const void* dq, const long long* dq_strides, const void* dk, const long long* dk_strides,
+                     void* dq_out, const long long* dq_out_strides, void* dk_out, const long long* dk_out_strides,
+                     const double* inv_freq, const int* axis, const int* positions, int axes, int B, int H, int H_kv, int N, int d,
+                     int rot_dim, float amplitude, int interleaved, int dtype, void* stream);
+
+/*
  * Frequencies of rotary positions, and their scaling for contexts longer than the trained one.  Host only.  With
  * f_i = base^(-2i / rot_dim), s = factor and n_i = trained_len f_i / (2 pi), how often pair i turns over the trained length:
  *     FA_ROPE_PLAIN     f_i                                         (factor and trained_len are ignored)
@@ -266,9 +287,12 @@ int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double 
 
 /*
  * A paged cache of keys and values.
- *   k_pages, v_pages : [n_pages, H_kv, page_size, d] of cache_dtype FA_BF16, FA_F16 or FA_FP8_E4M3, contiguous
+ *   k_pages, v_pages : [n_pages, H_kv, page_size, d] of cache_dtype FA_BF16, FA_F16 or FA_FP8_E4M3, contiguous; with FA_FP4_E2M1
+ *                 [n_pages, H_kv, page_size, d / 2] bytes of two codes, element 2i in the lower half of byte i
  *   k_scales, v_scales : fp32 [n_pages, H_kv, page_size] with FA_FP8_E4M3, where the cached value is code * scale of its
- *                 token and head; NULL otherwise (given with a 16-bit cache: FA_ERR_DTYPE)
+ *                 token and head; bytes [n_pages, H_kv, page_size, d / 32] with FA_FP4_E2M1 (aligned to 4), where it is
+ *                 code * 2^(byte - 127) of its 32 elements, and NaN with the byte 255; NULL otherwise (given with a 16-bit cache:
+ *                 FA_ERR_DTYPE)
  *   block_table : int32 [B, max_pages]; token p of sequence b is in slot p % page_size of page block_table[b][p / page_size]
  *   lens        : int32 [B], how many tokens of a sequence the cache holds (less than 0: none)
  * all on the device.  page_size: a multiple of 16 (else FA_ERR_UNSUPPORTED) with 4 page_size d <= 0x7ff00000; a cache that is
@@ -285,11 +309,14 @@ int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double 
  * In an e4m3 cache a token of one head gets
  *     scale = a / 448,   code = round-to-nearest-even e4m3 of clamp(x * (448 / a), +-448),   a = max |x| over its finite elements
  * (a = 0: scale 1; 0 < a < 2^-100: a = 2^-100).  So an infinity becomes the largest value of the token, and a NaN stays one.
+ * In an e2m1 cache each 32 elements of a row get
+ *     scale = the least power of two s >= 2^-100 with a <= 7 s,   code = round-to-nearest-even e2m1 of clamp(x / s, +-6),   a as above
+ * of those 32.  So no element is off by more than half a step, an infinity becomes +-6 s, and a NaN makes the byte of its scale 255.
  */
 #define FA_CACHE_MAX_PLACES 0x7fff0000
 
 int fa_cache_write(const void* k, const long long* k_strides, const void* v, const long long* v_strides,
-                   void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                   void* k_pages, void* v_pages, void* k_scales, void* v_scales,
                    const int* block_table, const int* lens, const int* counts, int B, int H_kv, int T, int d,
                    int page_size, int n_pages, int max_pages, int in_dtype, int cache_dtype, void* stream);
 
@@ -299,9 +326,58 @@ int fa_cache_write(const void* k, const long long* k_strides, const void* v, con
  *             as they are
  * out_dtype: FA_F32, FA_BF16 or FA_F16; a 16-bit cache is read as its own type or FA_F32 (else FA_ERR_UNSUPPORTED).
  */
-int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+int fa_cache_read(const void* k_pages, const void* v_pages, const void* k_scales, const void* v_scales,
                   const int* block_table, const int* lens, void* k, void* v, int B, int H_kv, int N, int d,
                   int page_size, int n_pages, int max_pages, int cache_dtype, int out_dtype, void* stream);
+
+/*
+ * Which pages of a pool belong to which sequence.  A page is in use if an entry of the block table names it, or held[page] is not 0
+ * (int32 [n_pages] on the device, or NULL: none), which is how a caller keeps pages that no row of the table has; it is free
+ * otherwise.  The calls below work on tables alone, on the device and in the caller's stream, and can be captured; where contents
+ * have to move they say which, and fa_cache_copy moves them, once for each layer whose pages go by the table.
+ *   missing   : int32 [1] (device, written): how many pages were asked for and not there.  Their entries are -1: no page.
+ *   src, dst  : int32 (device, written): the contents of page src[i] belong into page dst[i] now; -1 and -1: nothing to do
+ *   workspace : device scratch of at least fa_cache_pages_workspace_bytes(B, n_pages) bytes (fa_cache_fork: B_new in place of B),
+ *               16-byte aligned, owned by the caller; calls that may run at the same time need one each
+ * B * max_pages < 2^31.  Outputs overlap nothing else, but for new_table of fa_cache_compact, which may be block_table.  Free pages are
+ * given in ascending order, to rows and their entries in order: the results are the same in every run.
+ *
+ * fa_cache_fork: the batch of the next step.  New sequence i continues old sequence parents[i] (outside 0 .. B - 1: it is empty):
+ * new_lens[i] is the old length, and row i of new_table has the old row's pages up to it and -1 behind.  Whole pages are shared.  Of a
+ * last page that is not full, the first new sequence keeps the page, if none has it as a whole one; the others get a free one each,
+ * and (src, dst)[i] says so.  So sequences branch, change places and end by their parents alone, and what no new sequence has is
+ * free.  (Pages that the old table has behind a sequence's length are not taken over.)  Contents are to be copied before anything is
+ * written to the new sequences.
+ *   parents   : int32 [B_new];  new_table: int32 [B_new, max_pages];  new_lens, src, dst: int32 [B_new]
+ *
+ * fa_cache_extend: pages for the tokens that come next.  Entries of the places lens[b] .. lens[b] + counts[b] - 1 that are no page (-1, or
+ * anything outside the pool) get a free one; block_table is changed in place.  Places past the table count as missing.
+ *   counts    : int32 [B], or NULL: T of every sequence (above T counts as T).  T > 0, B * T < 2^31.
+ *
+ * fa_cache_compact: pages in use moved to the lowest numbers: the highest goes to the lowest free one, the next to the next, as long as
+ * that is lower, and `moves` times at most.  new_table is block_table by the new numbers.  Held pages stay where they are.  No page is
+ * a source and a destination.
+ *   src, dst  : int32 [moves], moves > 0 (n_pages / 2 are always enough);  top: int32 [1], one more than the highest page then in use
+ */
+size_t fa_cache_pages_workspace_bytes(int B, int n_pages);
+
+int fa_cache_fork(const int* block_table, const int* lens, const int* parents, const int* held, int* new_table, int* new_lens,
+                  int* src, int* dst, int* missing, void* workspace, size_t workspace_bytes, int B, int B_new, int page_size,
+                  int n_pages, int max_pages, void* stream);
+
+int fa_cache_extend(int* block_table, const int* lens, const int* counts, const int* held, int* missing, void* workspace,
+                    size_t workspace_bytes, int B, int T, int page_size, int n_pages, int max_pages, void* stream);
+
+int fa_cache_compact(const int* block_table, const int* held, int* new_table, int* src, int* dst, int* top, void* workspace,
+                     size_t workspace_bytes, int B, int moves, int n_pages, int max_pages, void* stream);
+
+/*
+ * Pages of a cache copied: src[i] to dst[i] for i < n, K and V with their scales.  A pair with a number outside the pool, or with the same
+ * twice, is left out.  No page may be dst twice, or dst of one pair and src of another: its contents are undefined then.
+ *   src, dst  : int32 [n] (device, read), n > 0; the cache as above, of any cache_dtype
+ */
+int fa_cache_copy(void* k_pages, void* v_pages, void* k_scales, void* v_scales, const int* src, const int* dst, int n,
+                  int H_kv, int d, int page_size, int n_pages, int cache_dtype, void* stream);
 
 /*
  * Attention of T new tokens of every sequence over the cache, which already holds their keys and values too (fa_cache_write
@@ -314,7 +390,7 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
  *   o       : the shape and dtype of q (device, written), strides as in fa_rope; lse : fp32 [B,H,T], contiguous (device, written)
  *             A row that sees nothing gets O = 0 and L = -infinity.  Rows of tokens from counts[b] on stay as they are.  o and
  *             lse overlap no other argument.
- *   cache_dtype : dtype, or FA_FP8_E4M3 (another: FA_ERR_UNSUPPORTED)
+ *   cache_dtype : dtype, FA_FP8_E4M3 or FA_FP4_E2M1 (another: FA_ERR_UNSUPPORTED)
  *   max_len : what lens[b] + T is expected to reach at most, or 0: max_pages * page_size.  It decides how the keys are
  *             divided over the chip and with that the time (far too large a number costs up to 1.7 times where all sequences are
  *             short), not which of them are seen.  fa_fwd_cache_workspace_bytes takes the same number, and max_pages * page_size
@@ -325,7 +401,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
  * has no influence on the row; an infinity or NaN in V that it sees makes its element of O one or the other.  Scores, softmax and
  * the sums are fp32.  For their product with V the probabilities are rounded to the 16-bit type of the cache, to two numbers of it
  * (a value and what that leaves out) with up to 16 rows (H / H_kv * T) to a key/value head; with FA_FP8_E4M3 the probabilities
- * times V's scales, which may have either sign, to two bf16 numbers always.  With p up to 2^8 for the largest of a row, sum p |v| and
+ * times V's scales, which may have either sign, to two bf16 numbers always.  With FA_FP4_E2M1 the cached values are bf16 numbers; fp16
+ * Q and the probabilities then go to their products as two bf16 numbers each.  With p up to 2^8 for the largest of a row, sum p |v| and
  * p times V's scales have to stay within fp32.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One
  * launch, or two where sequences are divided.
  */
@@ -334,7 +411,7 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const float* k_scale
 size_t fa_fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype);
 
 int fa_fwd_cache(const void* q, const long long* q_strides, const void* k_pages, const void* v_pages,
-                 const float* k_scales, const float* v_scales, const int* block_table, const int* lens, const int* counts,
+                 const void* k_scales, const void* v_scales, const int* block_table, const int* lens, const int* counts,
                  const int* tree, int tree_batches, void* o, const long long* o_strides, float* lse,
                  void* workspace, size_t workspace_bytes, int B, int H, int H_kv, int T, int d,
                  int page_size, int n_pages, int max_pages, int max_len, float scale, int dtype, int cache_dtype,

@@ -1,7 +1,8 @@
 """fp64 oracle of rotary positions, the paged cache and attention over it, sequence by sequence from the definitions.
 
 Arrays are numpy; a cache is a dict with k_pages, v_pages [n_pages, H_kv, page_size, d] (float64 values, or e4m3 codes as
-uint8 with k_scales, v_scales [n_pages, H_kv, page_size]) and block_table [B, max_pages].
+uint8 with k_scales, v_scales [n_pages, H_kv, page_size], or [.., d / 2] pairs of e2m1 codes as uint8 with scales [.., d / 32] as
+uint8) and block_table [B, max_pages].
 """
 import numpy as np
 
@@ -17,6 +18,20 @@ def rope(x, inv_freq, positions, rot_dim, interleaved, amplitude=1.0, transposed
     a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + rot_dim // 2)
     y[..., a] = x[..., a] * c - x[..., b] * s
     y[..., b] = x[..., a] * s + x[..., b] * c
+    return y
+
+
+def rope_axes(x, inv_freq, axis, positions, rot_dim, interleaved, amplitude=1.0, transposed=False):
+    """rope() with pair i turned by positions[axis[i]] (positions [axes,B,N]; an axis that there is not: by nothing)"""
+    positions = np.asarray(positions, dtype=np.float64)
+    at = np.stack([positions[a] if 0 <= a < len(positions) else 0 * positions[0] for a in axis], axis=-1)  # [B,N,pairs]
+    phi = at[:, None] * np.asarray(inv_freq, dtype=np.float64)
+    turn = amplitude * np.exp(1j * phi * (-1.0 if transposed else 1.0))
+    y = np.array(x, dtype=np.float64)
+    i = np.arange(rot_dim // 2)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + rot_dim // 2)
+    z = (x[..., a] + 1j * x[..., b]) * turn
+    y[..., a], y[..., b] = z.real, z.imag
     return y
 
 
@@ -46,6 +61,43 @@ def quantise_rows(x):
     return np.where(np.isnan(z), np.uint8(0x7F), codes).astype(np.uint8), (safe / np.float32(448)).astype(np.float32)
 
 
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def e2m1_encode(y):
+    """Codes of values: the nearest magnitude, in the middle of two the one of even code, at most 6; a NaN: any"""
+    y = np.nan_to_num(np.asarray(y, dtype=np.float64), nan=0.0, posinf=6.0, neginf=-6.0)
+    size = np.minimum(np.abs(y), 6.0)
+    below = np.clip(np.searchsorted(E2M1, size, side="right") - 1, 0, 6)
+    middle = (E2M1[below] + E2M1[below + 1]) / 2
+    code = np.where((size > middle) | ((size == middle) & (below % 2 == 1)), below + 1, below)
+    return (code + 8 * np.signbit(y)).astype(np.uint8)
+
+
+def e2m1_decode(code):
+    code = np.asarray(code)
+    return np.where(code & 8, -1.0, 1.0) * E2M1[code & 7]
+
+
+def quantise_groups(x):
+    """Pairs of codes (uint8 [..., d / 2]) and scales (uint8 [..., d / 32]) of x [..., d], as a 4-bit cache defines them."""
+    g = np.asarray(x, dtype=np.float64).reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
+    a = np.where(np.isfinite(g), np.abs(g), 0.0).max(axis=-1)
+    e = np.full(a.shape, -100)
+    for n in range(-100, 128):  # the least power of two with a <= 7 of it
+        e = np.where(a > 7 * 2.0 ** n, n + 1, e)
+    codes = e2m1_encode(g / (2.0 ** e.astype(np.float64))[..., None]).reshape(x.shape)
+    return codes[..., 0::2] | codes[..., 1::2] << 4, np.where(np.isnan(g).any(axis=-1), 255, e + 127).astype(np.uint8)
+
+
+def group_values(codes, scales):
+    """float64 [..., d] of pairs of codes and scales"""
+    x = e2m1_decode(np.stack((codes & 15, codes >> 4), axis=-1).reshape(codes.shape[:-1] + (2 * codes.shape[-1],)))
+    with np.errstate(over="ignore"):
+        s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return x * np.repeat(s, 32, axis=-1)
+
+
 def place(cache, b, p):
     """(page, slot) of place p of sequence b, or None"""
     n_pages, _, page_size, _ = cache["k_pages"].shape
@@ -63,6 +115,8 @@ def values(cache, name, places):
     rows = pages[at[:, 0], :, at[:, 1]]
     if pages.dtype != np.uint8:
         return rows.astype(np.float64)
+    if cache[name + "_scales"].dtype == np.uint8:
+        return group_values(rows, cache[name + "_scales"][at[:, 0], :, at[:, 1]])
     return fp8_oracle.e4m3_decode(rows) * cache[name + "_scales"][at[:, 0], :, at[:, 1]].astype(np.float64)[..., None]
 
 

@@ -22,13 +22,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfa_mi355.so")
 
 FA_OK = 0
-FA_F32, FA_BF16, FA_F16, FA_FP8_E4M3 = 0, 1, 2, 3
+FA_F32, FA_BF16, FA_F16, FA_FP8_E4M3, FA_FP4_E2M1 = 0, 1, 2, 3, 4
 _DTYPE_CODE = {torch.float32: FA_F32, torch.bfloat16: FA_BF16, torch.float16: FA_F16}
 
 EXPORTS = ("fa_fwd", "fa_fwd_fp8", "fa_fp8_quant_hadamard", "fa_bwd_workspace_bytes", "fa_bwd",
            "fa_fwd_schedule", "fa_fwd_gqa", "fa_fwd_fp8_gqa", "fa_bwd_gqa", "fa_bwd_noalloc", "fa_fwd_kernel_name",
            "fa_probe_mfma_flops", "fa_probe_mfma", "fa_status_string", "fa_rope", "fa_rope_bwd", "fa_rope_frequencies",
-           "fa_cache_write", "fa_cache_read", "fa_fwd_cache_workspace_bytes", "fa_fwd_cache")
+           "fa_cache_write", "fa_cache_read", "fa_fwd_cache_workspace_bytes", "fa_fwd_cache", "fa_rope_axes", "fa_rope_axes_bwd",
+           "fa_cache_pages_workspace_bytes", "fa_cache_fork", "fa_cache_extend", "fa_cache_compact", "fa_cache_copy")
 
 _lib = None
 
@@ -87,6 +88,15 @@ def lib():
         L.fa_fwd_cache_workspace_bytes.restype = ctypes.c_size_t
         L.fa_fwd_cache.argtypes = [vp, sp, vp, vp, fp, fp, ip, ip, ip, ip, ci, vp, sp, fp, vp, ctypes.c_size_t] + [ci] * 9 + [cf, ci, ci, vp]
         L.fa_fwd_cache.restype = ci
+        L.fa_rope_axes.argtypes = L.fa_rope_axes_bwd.argtypes = [vp, sp] * 4 + [vp, ip, ip] + [ci] * 7 + [cf, ci, ci, vp]
+        L.fa_rope_axes.restype = L.fa_rope_axes_bwd.restype = ci
+        L.fa_cache_pages_workspace_bytes.argtypes = [ci] * 2
+        L.fa_cache_pages_workspace_bytes.restype = ctypes.c_size_t
+        L.fa_cache_fork.argtypes = [ip] * 9 + [vp, ctypes.c_size_t] + [ci] * 5 + [vp]
+        L.fa_cache_extend.argtypes = [ip] * 5 + [vp, ctypes.c_size_t] + [ci] * 5 + [vp]
+        L.fa_cache_compact.argtypes = [ip] * 6 + [vp, ctypes.c_size_t] + [ci] * 4 + [vp]
+        L.fa_cache_copy.argtypes = [vp] * 4 + [ip] * 2 + [ci] * 6 + [vp]
+        L.fa_cache_fork.restype = L.fa_cache_extend.restype = L.fa_cache_compact.restype = L.fa_cache_copy.restype = ci
         L.fa_status_string.argtypes = [ci]
         L.fa_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -94,7 +104,9 @@ def lib():
             _native.bind(*(ctypes.cast(f, vp).value for f in (L.fa_fwd_gqa, L.fa_fwd_fp8_gqa, L.fa_fp8_quant_hadamard,
                                                               L.fa_bwd_workspace_bytes, L.fa_bwd_gqa, L.fa_rope, L.fa_rope_bwd,
                                                               L.fa_cache_write, L.fa_cache_read, L.fa_fwd_cache_workspace_bytes,
-                                                              L.fa_fwd_cache)))
+                                                              L.fa_fwd_cache, L.fa_rope_axes, L.fa_rope_axes_bwd,
+                                                              L.fa_cache_pages_workspace_bytes, L.fa_cache_fork, L.fa_cache_extend,
+                                                              L.fa_cache_compact, L.fa_cache_copy)))
     return _lib
 
 
@@ -347,9 +359,12 @@ def fa_rope_frequencies(rot_dim, base=10000.0, scaling=FA_ROPE_PLAIN, factor=1.0
     return f.to(device), amplitude.value
 
 
-def _rope(name, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out):
+def _rope(name, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, axis=None, several=False):
     if _native is not None:
-        r = _native.rope(name == "fa_rope_bwd", q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, _stream)
+        if several:
+            r = _native.rope_axes(name == "fa_rope_axes_bwd", q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, _stream, axis)
+        else:
+            r = _native.rope(name == "fa_rope_bwd", q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, _stream)
         if r is not None:
             return _outputs(r, name)
     if q.dim() != 4 or (k is not None and k.dim() != 4):
@@ -360,7 +375,12 @@ def _rope(name, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_ou
     dtypes = (q.dtype,) if q.dtype in _DTYPE_CODE else tuple(_DTYPE_CODE)
     _check("q", q, q.shape, dtypes, strided=True)
     _check("inv_freq", inv_freq, (rot_dim // 2,), (torch.float64,))
-    if positions is not None:
+    if several:
+        if positions.dim() != 3:
+            raise ValueError("positions must be [axes,B,N]")
+        _check("axis", axis, (rot_dim // 2,), (torch.int32,))
+        _check("positions", positions, (positions.shape[0], B, N), (torch.int32,))
+    elif positions is not None:
         _check("positions", positions, (B, N), (torch.int32,))
     if q_out is None:
         q_out = _empty_like(q, q.dtype)
@@ -372,8 +392,9 @@ def _rope(name, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_ou
         _check("k_out", k_out, k.shape, dtypes, strided=True)
     else:
         k_out = None
+    turns = (_ptr(axis), _ptr(positions), positions.shape[0]) if several else (_ptr(positions),)
     st = getattr(lib(), name)(q.data_ptr(), _strides(q), _ptr(k), None if k is None else _strides(k), q_out.data_ptr(), _strides(q_out),
-                              _ptr(k_out), None if k is None else _strides(k_out), inv_freq.data_ptr(), _ptr(positions), B, H, H_kv, N, d,
+                              _ptr(k_out), None if k is None else _strides(k_out), inv_freq.data_ptr(), *turns, B, H, H_kv, N, d,
                               rot_dim, float(amplitude), int(bool(interleaved)), _DTYPE_CODE[q.dtype], _stream())
     if st != FA_OK:
         raise FaError(st, name)
@@ -392,23 +413,52 @@ def fa_rope_bwd(dq, inv_freq, k=None, positions=None, rot_dim=None, interleaved=
     return _rope("fa_rope_bwd", dq, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out)
 
 
+def fa_rope_axes(q, inv_freq, axis, positions, k=None, rot_dim=None, interleaved=False, amplitude=1.0, q_out=None, k_out=None):
+    """fa_rope with several axes: pair i goes by positions[axis[i]] (positions int32 [axes,B,N], axis int32 [rot_dim / 2])."""
+    return _rope("fa_rope_axes", q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, axis, True)
+
+
+def fa_rope_axes_bwd(dq, inv_freq, axis, positions, k=None, rot_dim=None, interleaved=False, amplitude=1.0, q_out=None, k_out=None):
+    """Gradients by the rotated q (and k, given as `k`) taken back to gradients by fa_rope_axes' inputs; arguments as there."""
+    return _rope("fa_rope_axes_bwd", dq, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, axis, True)
+
+
 _CACHE_CODE = {torch.bfloat16: FA_BF16, torch.float16: FA_F16, torch.uint8: FA_FP8_E4M3, torch.float8_e4m3fn: FA_FP8_E4M3}
+
+
+_POWERS = (torch.uint8, torch.float8_e8m0fnu)
+
+
+def _in_four_bits(k_pages, k_scales):
+    """Whether the last dimension of pages is half of d: two e2m1 codes to a byte, which their type says, or that of the scales does"""
+    return k_pages.dtype is torch.float4_e2m1fn_x2 or (k_pages.dtype is torch.uint8 and k_scales is not None and k_scales.dtype in _POWERS)
+
+
+def _check_pages(H_kv, d, k_pages, v_pages, k_scales, v_scales):
+    """(page_size, n_pages, dtype code) of pages and scales that belong together"""
+    if k_pages.dim() != 4:
+        raise ValueError("pages must be [n_pages,H_kv,page_size,d]")
+    n_pages, _, page_size, _ = k_pages.shape
+    four = _in_four_bits(k_pages, k_scales)
+    dtypes = (k_pages.dtype,) if four or k_pages.dtype in _CACHE_CODE else tuple(_CACHE_CODE)
+    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        _check(name, t, (n_pages, H_kv, page_size, d // 2 if four else d), dtypes)
+    code = FA_FP4_E2M1 if four else _CACHE_CODE[k_pages.dtype]
+    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+        if (t is not None) != (code in (FA_FP8_E4M3, FA_FP4_E2M1)):
+            raise ValueError("an e4m3 or e2m1 cache has k_scales and v_scales, a 16-bit one has none")
+        if four:
+            _check(name, t, (n_pages, H_kv, page_size, d // 32), _POWERS)
+        elif t is not None:
+            _check(name, t, (n_pages, H_kv, page_size), (torch.float32,))
+    return page_size, n_pages, code
 
 
 def _check_cache(B, H_kv, d, k_pages, v_pages, block_table, lens, counts, k_scales, v_scales):
     """(page_size, n_pages, max_pages, dtype code) of a cache whose tensors belong together"""
     if k_pages.dim() != 4 or block_table.dim() != 2:
         raise ValueError("pages must be [n_pages,H_kv,page_size,d] and the block table [B,max_pages]")
-    n_pages, _, page_size, _ = k_pages.shape
-    dtypes = (k_pages.dtype,) if k_pages.dtype in _CACHE_CODE else tuple(_CACHE_CODE)
-    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-        _check(name, t, (n_pages, H_kv, page_size, d), dtypes)
-    code = _CACHE_CODE[k_pages.dtype]
-    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
-        if (t is not None) != (code == FA_FP8_E4M3):
-            raise ValueError("an e4m3 cache has k_scales and v_scales, a 16-bit one has none")
-        if t is not None:
-            _check(name, t, (n_pages, H_kv, page_size), (torch.float32,))
+    page_size, n_pages, code = _check_pages(H_kv, d, k_pages, v_pages, k_scales, v_scales)
     _check("block_table", block_table, (B, block_table.shape[1]), (torch.int32,))
     _check("lens", lens, (B,), (torch.int32,))
     if counts is not None:
@@ -418,7 +468,9 @@ def _check_cache(B, H_kv, d, k_pages, v_pages, block_table, lens, counts, k_scal
 
 def fa_cache_write(k, v, k_pages, v_pages, block_table, lens, counts=None, k_scales=None, v_scales=None):
     """k, v [B,H_kv,T,d] (contiguous rows) into the cache behind the lens[b] tokens that it holds: T of every sequence, or
-    counts[b] of them.  Pages [n_pages,H_kv,page_size,d]: 16-bit, or e4m3 codes (uint8 or float8_e4m3fn) with scales."""
+    counts[b] of them.  Pages [n_pages,H_kv,page_size,d]: 16-bit, or e4m3 codes (uint8 or float8_e4m3fn) with scales; or
+    [n_pages,H_kv,page_size,d / 2] of two e2m1 codes each (uint8 or float4_e2m1fn_x2), with scales [n_pages,H_kv,page_size,d / 32]
+    that are powers of two (uint8 or float8_e8m0fnu)."""
     if _native is not None:
         r = _native.cache_write(k, v, k_pages, v_pages, block_table, lens, counts, k_scales, v_scales, _stream)
         if r is not None:
@@ -448,6 +500,8 @@ def fa_cache_read(k_pages, v_pages, block_table, lens, N=None, dtype=None, k_sca
     if k_pages.dim() != 4 or block_table.dim() != 2:
         raise ValueError("pages must be [n_pages,H_kv,page_size,d] and the block table [B,max_pages]")
     B, (_, H_kv, _, d) = block_table.shape[0], k_pages.shape
+    if _in_four_bits(k_pages, k_scales):
+        d *= 2
     given = k if k is not None else v
     if given is not None:
         N, dtype = given.shape[2] if N is None else int(N), given.dtype if dtype is None else dtype
@@ -469,6 +523,120 @@ def fa_cache_read(k_pages, v_pages, block_table, lens, N=None, dtype=None, k_sca
     if st != FA_OK:
         raise FaError(st, "fa_cache_read")
     return k, v
+
+
+def _new(t, shape):
+    return torch.empty(shape, device=t.device, dtype=torch.int32)
+
+
+def fa_cache_pages_workspace_bytes(B, n_pages):
+    return int(lib().fa_cache_pages_workspace_bytes(B, n_pages))
+
+
+def _pages_workspace(workspace, B, n_pages, like):
+    if workspace is None:
+        return torch.empty((fa_cache_pages_workspace_bytes(B, n_pages),), device=like.device, dtype=torch.uint8)
+    _check("workspace", workspace, (workspace.numel(),), (torch.uint8,))
+    return workspace
+
+
+def _check_ints(*named):
+    for name, t, shape in named:
+        if t is not None:
+            _check(name, t, shape, (torch.int32,))
+
+
+def _check_table(block_table):
+    if block_table.dim() != 2:
+        raise ValueError("the block table must be [B,max_pages]")
+    _check("block_table", block_table, block_table.shape, (torch.int32,))
+
+
+def fa_cache_fork(block_table, lens, parents, page_size, n_pages, held=None, new_table=None, new_lens=None, src=None, dst=None, missing=None,
+                  workspace=None):
+    """The batch of the next step: new_table [B_new,max_pages] and new_lens of sequences that continue parents[i] (int32 [B_new]; none: -1),
+    sharing whole pages; what fa_cache_copy has to copy for them (src, dst); and how many pages were missing."""
+    if _native is not None:
+        r = _native.cache_fork(block_table, lens, parents, page_size, n_pages, held, new_table, new_lens, src, dst, missing, workspace, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_fork")
+    _check_table(block_table)
+    if parents.dim() != 1:
+        raise ValueError("parents must be [B_new]")
+    (B, max_pages), B_new, n_pages = block_table.shape, parents.shape[0], int(n_pages)
+    _check_ints(("lens", lens, (B,)), ("parents", parents, (B_new,)), ("held", held, (n_pages,)))
+    new_table = _new(block_table, (B_new, max_pages)) if new_table is None else new_table
+    new_lens, src, dst = (_new(block_table, (B_new,)) if t is None else t for t in (new_lens, src, dst))
+    missing = _new(block_table, (1,)) if missing is None else missing
+    _check_ints(("new_table", new_table, (B_new, max_pages)), ("new_lens", new_lens, (B_new,)), ("src", src, (B_new,)), ("dst", dst, (B_new,)),
+                ("missing", missing, (1,)))
+    workspace = _pages_workspace(workspace, B_new, n_pages, block_table)
+    st = lib().fa_cache_fork(block_table.data_ptr(), lens.data_ptr(), parents.data_ptr(), _ptr(held), new_table.data_ptr(), new_lens.data_ptr(),
+                             src.data_ptr(), dst.data_ptr(), missing.data_ptr(), workspace.data_ptr(), workspace.numel(), B, B_new, int(page_size),
+                             n_pages, max_pages, _stream())
+    if st != FA_OK:
+        raise FaError(st, "fa_cache_fork")
+    return new_table, new_lens, src, dst, missing
+
+
+def fa_cache_extend(block_table, lens, T, page_size, n_pages, counts=None, held=None, missing=None, workspace=None):
+    """Free pages for the next T (or counts[b]) tokens of every sequence, where block_table, which is changed in place, has none.  Returns
+    it, and how many were missing."""
+    if _native is not None:
+        r = _native.cache_extend(block_table, lens, T, page_size, n_pages, counts, held, missing, workspace, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_extend")
+    _check_table(block_table)
+    (B, max_pages), n_pages = block_table.shape, int(n_pages)
+    missing = _new(block_table, (1,)) if missing is None else missing
+    _check_ints(("lens", lens, (B,)), ("counts", counts, (B,)), ("held", held, (n_pages,)), ("missing", missing, (1,)))
+    workspace = _pages_workspace(workspace, B, n_pages, block_table)
+    st = lib().fa_cache_extend(block_table.data_ptr(), lens.data_ptr(), _ptr(counts), _ptr(held), missing.data_ptr(), workspace.data_ptr(),
+                               workspace.numel(), B, int(T), int(page_size), n_pages, max_pages, _stream())
+    if st != FA_OK:
+        raise FaError(st, "fa_cache_extend")
+    return block_table, missing
+
+
+def fa_cache_compact(block_table, n_pages, moves=None, held=None, new_table=None, src=None, dst=None, top=None, workspace=None):
+    """Pages in use moved to the lowest numbers, `moves` of them at most (None: n_pages / 2, which is always enough): the table by the new
+    numbers (new_table may be block_table), what fa_cache_copy has to copy (src, dst [moves]), and one more than the highest page in use."""
+    if _native is not None:
+        r = _native.cache_compact(block_table, n_pages, moves, held, new_table, src, dst, top, workspace, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_compact")
+    _check_table(block_table)
+    (B, max_pages), n_pages = block_table.shape, int(n_pages)
+    moves = max(n_pages // 2, 1) if moves is None else int(moves)
+    _check_ints(("held", held, (n_pages,)))
+    new_table = _new(block_table, (B, max_pages)) if new_table is None else new_table
+    src, dst = (_new(block_table, (moves,)) if t is None else t for t in (src, dst))
+    top = _new(block_table, (1,)) if top is None else top
+    _check_ints(("new_table", new_table, (B, max_pages)), ("src", src, (moves,)), ("dst", dst, (moves,)), ("top", top, (1,)))
+    workspace = _pages_workspace(workspace, B, n_pages, block_table)
+    st = lib().fa_cache_compact(block_table.data_ptr(), _ptr(held), new_table.data_ptr(), src.data_ptr(), dst.data_ptr(), top.data_ptr(),
+                                workspace.data_ptr(), workspace.numel(), B, moves, n_pages, max_pages, _stream())
+    if st != FA_OK:
+        raise FaError(st, "fa_cache_compact")
+    return new_table, src, dst, top
+
+
+def fa_cache_copy(k_pages, v_pages, src, dst, k_scales=None, v_scales=None):
+    """Page src[i] of a cache (any that fa_cache_write takes) copied to page dst[i], K and V with their scales; pairs of -1 are left out."""
+    if _native is not None:
+        r = _native.cache_copy(k_pages, v_pages, src, dst, k_scales, v_scales, _stream)
+        if r is not None:
+            return _outputs(r, "fa_cache_copy")
+    if k_pages.dim() != 4 or src.dim() != 1:
+        raise ValueError("pages must be [n_pages,H_kv,page_size,d], src and dst [n]")
+    H_kv, d = k_pages.shape[1], k_pages.shape[3] * (2 if _in_four_bits(k_pages, k_scales) else 1)
+    page_size, n_pages, code = _check_pages(H_kv, d, k_pages, v_pages, k_scales, v_scales)
+    _check_ints(("src", src, (src.shape[0],)), ("dst", dst, (src.shape[0],)))
+    st = lib().fa_cache_copy(k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), src.data_ptr(), dst.data_ptr(), src.shape[0],
+                             H_kv, d, page_size, n_pages, code, _stream())
+    if st != FA_OK:
+        raise FaError(st, "fa_cache_copy")
+    return k_pages, v_pages
 
 
 def fa_tree_words(visible):

@@ -36,6 +36,12 @@ struct {
     decltype(&fa_cache_read) cache_read;
     decltype(&fa_fwd_cache_workspace_bytes) cache_workspace_bytes;
     decltype(&fa_fwd_cache) fwd_cache;
+    decltype(&fa_rope_axes) rope_axes, rope_axes_bwd;
+    decltype(&fa_cache_pages_workspace_bytes) pages_workspace_bytes;
+    decltype(&fa_cache_fork) cache_fork;
+    decltype(&fa_cache_extend) cache_extend;
+    decltype(&fa_cache_compact) cache_compact;
+    decltype(&fa_cache_copy) cache_copy;
 } lib;
 
 // The arguments of a call; `ok` turns false at the first that is not as the native way takes it.
@@ -327,10 +333,11 @@ T* pointer(const at::Tensor* t) {
     return t ? static_cast<T*>(t->data_ptr()) : nullptr;
 }
 
-// (backward, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, stream)
-PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+// (backward, q, inv_freq, k, positions, rot_dim, interleaved, amplitude, q_out, k_out, stream); with several axes, their numbers too
+template <bool AXES>
+PyObject* rope_any(PyObject* const* args, Py_ssize_t n) {
     return native([&]() -> PyObject* {
-        Arguments a(args, n, 11);
+        Arguments a(args, n, AXES ? 12 : 11);
         const int backward = a.flag(0), interleaved = a.flag(6);
         const double amplitude = a.number(7);
         Shape s, sk = {};
@@ -350,7 +357,18 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor* f = fitting(a, 2, device, {rot_dim / 2}, at::kDouble);
         const at::Tensor* k = a.given(3) ? four(a, 3, sk) : nullptr;
         if (k) fitting(a, 3, device, {s.B, sk.H, s.N, s.d}, type, &ks);
-        const at::Tensor* positions = a.given(4) ? fitting(a, 4, device, {s.B, s.N}, at::kInt) : nullptr;
+        const at::Tensor *positions = nullptr, *axis = nullptr;
+        int axes = 0;
+        if constexpr (AXES) {
+            if (!a.ok || !THPVariable_CheckExact(args[4])) return nullptr;
+            const at::Tensor& t = THPVariable_Unpack(args[4]);
+            if (!t.defined() || t.dim() != 3 || t.size(0) > 0x7fffffff) return nullptr;
+            axes = (int)t.size(0);
+            positions = fitting(a, 4, device, {axes, s.B, s.N}, at::kInt);
+            axis = fitting(a, 11, device, {rot_dim / 2}, at::kInt);
+        } else if (a.given(4)) {
+            positions = fitting(a, 4, device, {s.B, s.N}, at::kInt);
+        }
         if (!a.ok || (!k && args[9] != Py_None)) return nullptr;
         void* stream = a.stream(10);
         const at::Tensor q_out = fitting_output(a, 8, device, q->sizes(), type, *q, &qos);
@@ -359,9 +377,14 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const void *qp = q->data_ptr(), *kp = pointer(k);
         void *qop = q_out.data_ptr(), *kop = k ? k_out.data_ptr() : nullptr;
         const double* fp = pointer<double>(f);
-        const int* pp = pointer<int>(positions);
-        const auto call = backward ? lib.rope_bwd : lib.rope;
+        const int *pp = pointer<int>(positions), *ap = pointer<int>(axis);
         const int st = without_gil([&] {
+            if constexpr (AXES) {
+                const auto call = backward ? lib.rope_axes_bwd : lib.rope_axes;
+                return call(qp, qs.p, kp, ks.p, qop, qos.p, kop, kos.p, fp, ap, pp, axes, s.B, s.H, sk.H, s.N, s.d, (int)rot_dim, (float)amplitude,
+                            interleaved, code, stream);
+            }
+            const auto call = backward ? lib.rope_bwd : lib.rope;
             return call(qp, qs.p, kp, ks.p, qop, qos.p, kop, kos.p, fp, pp, s.B, s.H, sk.H, s.N, s.d, (int)rot_dim, (float)amplitude,
                         interleaved, code, stream);
         });
@@ -369,37 +392,68 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// The tensors of a cache, from argument `at` on: k_pages, v_pages, block_table, lens; scales and counts where they stand
-struct CacheArguments {
-    const at::Tensor *k, *v, *table, *lens, *k_scales, *v_scales, *counts;
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) { return rope_any<false>(args, n); }
+PyObject* rope_axes(PyObject*, PyObject* const* args, Py_ssize_t n) { return rope_any<true>(args, n); }
+
+// Pages and scales from argument `at`, `k_scales` and `v_scales` on: whether they belong together, what they hold, and of 4-bit ones
+// the whole d
+struct PagesArguments {
+    const at::Tensor *k, *v, *k_scales, *v_scales;
     Shape s;  // n_pages, H_kv, page_size, d
-    int code, max_pages;
+    int code;
 };
-bool cache_arguments(Arguments& a, CacheArguments& c, int device, Py_ssize_t at, int B, Py_ssize_t k_scales, Py_ssize_t v_scales, Py_ssize_t counts) {
+bool pages_arguments(Arguments& a, PagesArguments& c, int device, Py_ssize_t at, Py_ssize_t k_scales, Py_ssize_t v_scales) {
+    auto of_powers = [&](Py_ssize_t i, at::ScalarType& type) {
+        if (!a.given(i) || !THPVariable_CheckExact(a.args[i])) return false;
+        type = THPVariable_Unpack(a.args[i]).scalar_type();
+        return type == at::kByte || type == at::kFloat8_e8m0fnu;
+    };
     c.k = four(a, at, c.s);
     if (!a.ok) return false;
     const at::ScalarType type = c.k->scalar_type();
+    at::ScalarType powers;
     switch (type) {
         case at::kBFloat16: c.code = FA_BF16; break;
         case at::kHalf: c.code = FA_F16; break;
-        case at::kByte:
+        case at::kByte: c.code = of_powers(k_scales, powers) ? FA_FP4_E2M1 : FA_FP8_E4M3; break;
+        case at::kFloat4_e2m1fn_x2: c.code = FA_FP4_E2M1; break;
         case at::kFloat8_e4m3fn: c.code = FA_FP8_E4M3; break;
         default: return a.ok = false;
     }
     fitting(a, at, device, c.k->sizes(), type);
     c.v = fitting(a, at + 1, device, c.k->sizes(), type);
-    if (!a.ok || !THPVariable_CheckExact(a.args[at + 2]) || THPVariable_Unpack(a.args[at + 2]).dim() != 2) return a.ok = false;
+    if (!a.ok) return false;
+    c.k_scales = c.v_scales = nullptr;
+    const bool scaled = c.code == FA_FP8_E4M3 || c.code == FA_FP4_E2M1;
+    if (a.given(k_scales) != scaled || a.given(v_scales) != scaled) return a.ok = false;
+    if (c.code == FA_FP8_E4M3) {
+        c.k_scales = fitting(a, k_scales, device, {c.s.B, c.s.H, c.s.N}, at::kFloat);
+        c.v_scales = fitting(a, v_scales, device, {c.s.B, c.s.H, c.s.N}, at::kFloat);
+    }
+    if (c.code == FA_FP4_E2M1) {
+        if (c.s.d > 0x3fffffff) return a.ok = false;
+        c.s.d *= 2;
+        if (!of_powers(k_scales, powers)) return a.ok = false;
+        c.k_scales = fitting(a, k_scales, device, {c.s.B, c.s.H, c.s.N, c.s.d / 32}, powers);
+        if (!of_powers(v_scales, powers)) return a.ok = false;
+        c.v_scales = fitting(a, v_scales, device, {c.s.B, c.s.H, c.s.N, c.s.d / 32}, powers);
+    }
+    return a.ok;
+}
+
+// The tensors of a cache, from argument `at` on: k_pages, v_pages, block_table, lens; scales and counts where they stand
+struct CacheArguments : PagesArguments {
+    const at::Tensor *table, *lens, *counts;
+    int max_pages;
+};
+bool cache_arguments(Arguments& a, CacheArguments& c, int device, Py_ssize_t at, int B, Py_ssize_t k_scales, Py_ssize_t v_scales, Py_ssize_t counts) {
+    if (!pages_arguments(a, c, device, at, k_scales, v_scales) || !THPVariable_CheckExact(a.args[at + 2]) || THPVariable_Unpack(a.args[at + 2]).dim() != 2) return a.ok = false;
     const int64_t wide = THPVariable_Unpack(a.args[at + 2]).size(1);
     if (wide > 0x7fffffff) return a.ok = false;
     c.max_pages = (int)wide;
     c.table = fitting(a, at + 2, device, {B, wide}, at::kInt);
     c.lens = fitting(a, at + 3, device, {B}, at::kInt);
-    c.k_scales = c.v_scales = c.counts = nullptr;
-    if (a.given(k_scales) != (c.code == FA_FP8_E4M3) || a.given(v_scales) != (c.code == FA_FP8_E4M3)) return a.ok = false;
-    if (c.code == FA_FP8_E4M3) {
-        c.k_scales = fitting(a, k_scales, device, {c.s.B, c.s.H, c.s.N}, at::kFloat);
-        c.v_scales = fitting(a, v_scales, device, {c.s.B, c.s.H, c.s.N}, at::kFloat);
-    }
+    c.counts = nullptr;
     if (counts >= 0 && a.given(counts)) c.counts = fitting(a, counts, device, {B}, at::kInt);
     return a.ok;
 }
@@ -422,7 +476,7 @@ PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!a.ok) return nullptr;
         const void *kp = k->data_ptr(), *vp = v->data_ptr();
         void *kpp = c.k->data_ptr(), *vpp = c.v->data_ptr();
-        float *ksp = pointer<float>(c.k_scales), *vsp = pointer<float>(c.v_scales);
+        void *ksp = pointer(c.k_scales), *vsp = pointer(c.v_scales);
         const int *tp = pointer<int>(c.table), *lp = pointer<int>(c.lens), *cp = pointer<int>(c.counts);
         const int st = without_gil([&] {
             return lib.cache_write(kp, ks.p, vp, vs.p, kpp, vpp, ksp, vsp, tp, lp, cp, s.B, s.H, s.N, s.d, c.s.N, c.s.B, c.max_pages, code,
@@ -444,7 +498,7 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!cache_arguments(a, c, device, 0, (int)B, 6, 7, -1)) return nullptr;
         const Py_ssize_t given = a.given(8) ? 8 : 9;
         Shape s = {(int)B, c.s.H, 0, c.s.d};
-        at::ScalarType type = c.code == FA_FP8_E4M3 ? at::kBFloat16 : c.k->scalar_type();
+        at::ScalarType type = c.code == FA_FP8_E4M3 || c.code == FA_FP4_E2M1 ? at::kBFloat16 : c.k->scalar_type();
         if (a.given(given)) {
             const at::Tensor* t = four(a, given, s);
             if (!a.ok) return nullptr;
@@ -474,7 +528,7 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor v = fitting_output(a, 9, device, {B, c.s.H, N, c.s.d}, type, *c.k);
         if (!a.ok) return nullptr;
         const void *kpp = c.k->data_ptr(), *vpp = c.v->data_ptr();
-        const float *ksp = pointer<float>(c.k_scales), *vsp = pointer<float>(c.v_scales);
+        const void *ksp = pointer(c.k_scales), *vsp = pointer(c.v_scales);
         const int *tp = pointer<int>(c.table), *lp = pointer<int>(c.lens);
         void *kp = k.data_ptr(), *vp = v.data_ptr();
         const int st = without_gil([&] {
@@ -523,7 +577,7 @@ PyObject* fwd_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
             workspace = at::empty({need}, q->options().dtype(at::kByte));
         }
         const void *qp = q->data_ptr(), *kpp = c.k->data_ptr(), *vpp = c.v->data_ptr();
-        const float *ksp = pointer<float>(c.k_scales), *vsp = pointer<float>(c.v_scales);
+        const void *ksp = pointer(c.k_scales), *vsp = pointer(c.v_scales);
         const int *tp = pointer<int>(c.table), *lp = pointer<int>(c.lens), *cp = pointer<int>(c.counts), *wp = pointer<int>(tree);
         void *op = o.data_ptr(), *space = workspace.defined() ? workspace.data_ptr() : nullptr;
         float* lsep = static_cast<float*>(lse.data_ptr());
@@ -536,13 +590,152 @@ PyObject* fwd_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// ---- Pages of a pool
+
+// Argument i as a whole number of int's range
+int whole(Arguments& a, Py_ssize_t i) {
+    if (!a.ok || !PyLong_CheckExact(a.args[i])) return a.ok = false;
+    const long x = PyLong_AsLong(a.args[i]);
+    if (x < 0 || x > 0x7fffffff) a.ok = false;  // (and an overflow's -1; Python's ints go through the Python way)
+    return (int)x;
+}
+// [B, max_pages]
+const at::Tensor* table_of(Arguments& a, Py_ssize_t i, int device, int& B, int& max_pages) {
+    if (!a.ok || !THPVariable_CheckExact(a.args[i])) {
+        a.ok = false;
+        return nullptr;
+    }
+    const at::Tensor& t = THPVariable_Unpack(a.args[i]);
+    if (!t.defined() || t.dim() != 2 || t.size(0) > 0x7fffffff || t.size(1) > 0x7fffffff) {
+        a.ok = false;
+        return nullptr;
+    }
+    B = (int)t.size(0);
+    max_pages = (int)t.size(1);
+    return fitting(a, i, device, {B, max_pages}, at::kInt);
+}
+const at::Tensor* ints_or_none(Arguments& a, Py_ssize_t i, int device, int64_t size) { return a.given(i) ? fitting(a, i, device, {size}, at::kInt) : nullptr; }
+at::Tensor pages_workspace(Arguments& a, Py_ssize_t i, int device, int B, int n_pages, const at::Tensor& like) {
+    if (!a.given(i)) return a.ok ? at::empty({(int64_t)lib.pages_workspace_bytes(B, n_pages)}, like.options().dtype(at::kByte)) : at::Tensor();
+    const at::Tensor* t = a.tensor(i);
+    if (!t || t->device().index() != device || t->scalar_type() != at::kByte || t->dim() != 1) {
+        a.ok = false;
+        return at::Tensor();
+    }
+    return *t;
+}
+
+// (block_table, lens, parents, page_size, n_pages, held, new_table, new_lens, src, dst, missing, workspace, stream)
+PyObject* cache_fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return native([&]() -> PyObject* {
+        Arguments a(args, n, 13);
+        if (!a.ok) return nullptr;
+        const int device = current_device();
+        int B = 0, max_pages = 0;
+        const at::Tensor* table = table_of(a, 0, device, B, max_pages);
+        const at::Tensor* lens = fitting(a, 1, device, {B}, at::kInt);
+        if (!a.ok || !THPVariable_CheckExact(args[2]) || THPVariable_Unpack(args[2]).dim() != 1) return nullptr;
+        const int64_t rows = THPVariable_Unpack(args[2]).size(0);
+        if (rows > 0x7fffffff) return nullptr;
+        const at::Tensor* parents = fitting(a, 2, device, {rows}, at::kInt);
+        const int page_size = whole(a, 3), n_pages = whole(a, 4), B_new = (int)rows;
+        const at::Tensor* held = ints_or_none(a, 5, device, n_pages);
+        void* stream = a.stream(12);
+        if (!a.ok) return nullptr;
+        const at::Tensor new_table = fitting_output(a, 6, device, {B_new, max_pages}, at::kInt, *table), new_lens = fitting_output(a, 7, device, {B_new}, at::kInt, *table),
+                         src = fitting_output(a, 8, device, {B_new}, at::kInt, *table), dst = fitting_output(a, 9, device, {B_new}, at::kInt, *table),
+                         missing = fitting_output(a, 10, device, {1}, at::kInt, *table);
+        const at::Tensor workspace = pages_workspace(a, 11, device, B_new, n_pages, *table);
+        if (!a.ok) return nullptr;
+        const int *tp = pointer<int>(table), *lp = pointer<int>(lens), *pp = pointer<int>(parents), *hp = pointer<int>(held);
+        int *ntp = pointer<int>(&new_table), *nlp = pointer<int>(&new_lens), *sp = pointer<int>(&src), *dp = pointer<int>(&dst), *mp = pointer<int>(&missing);
+        void* wp = workspace.data_ptr();
+        const size_t bytes = (size_t)workspace.numel();
+        const int st = without_gil([&] {
+            return lib.cache_fork(tp, lp, pp, hp, ntp, nlp, sp, dp, mp, wp, bytes, B, B_new, page_size, n_pages, max_pages, stream);
+        });
+        return result(st, a, {6, 7, 8, 9, 10}, {new_table, new_lens, src, dst, missing});
+    });
+}
+
+// (block_table, lens, T, page_size, n_pages, counts, held, missing, workspace, stream)
+PyObject* cache_extend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return native([&]() -> PyObject* {
+        Arguments a(args, n, 10);
+        if (!a.ok) return nullptr;
+        const int device = current_device();
+        int B = 0, max_pages = 0;
+        const at::Tensor* table = table_of(a, 0, device, B, max_pages);
+        const at::Tensor* lens = fitting(a, 1, device, {B}, at::kInt);
+        const int T = whole(a, 2), page_size = whole(a, 3), n_pages = whole(a, 4);
+        const at::Tensor *counts = ints_or_none(a, 5, device, B), *held = ints_or_none(a, 6, device, n_pages);
+        void* stream = a.stream(9);
+        if (!a.ok) return nullptr;
+        const at::Tensor missing = fitting_output(a, 7, device, {1}, at::kInt, *table);
+        const at::Tensor workspace = pages_workspace(a, 8, device, B, n_pages, *table);
+        if (!a.ok) return nullptr;
+        int *tp = pointer<int>(table), *mp = pointer<int>(&missing);
+        const int *lp = pointer<int>(lens), *cp = pointer<int>(counts), *hp = pointer<int>(held);
+        void* wp = workspace.data_ptr();
+        const size_t bytes = (size_t)workspace.numel();
+        const int st = without_gil([&] { return lib.cache_extend(tp, lp, cp, hp, mp, wp, bytes, B, T, page_size, n_pages, max_pages, stream); });
+        return result(st, a, {0, 7}, {*table, missing});
+    });
+}
+
+// (block_table, n_pages, moves, held, new_table, src, dst, top, workspace, stream)
+PyObject* cache_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return native([&]() -> PyObject* {
+        Arguments a(args, n, 10);
+        if (!a.ok) return nullptr;
+        const int device = current_device();
+        int B = 0, max_pages = 0;
+        const at::Tensor* table = table_of(a, 0, device, B, max_pages);
+        const int n_pages = whole(a, 1), moves = a.given(2) ? whole(a, 2) : n_pages > 1 ? n_pages / 2 : 1;
+        const at::Tensor* held = ints_or_none(a, 3, device, n_pages);
+        void* stream = a.stream(9);
+        if (!a.ok) return nullptr;
+        const at::Tensor new_table = fitting_output(a, 4, device, {B, max_pages}, at::kInt, *table), src = fitting_output(a, 5, device, {moves}, at::kInt, *table),
+                         dst = fitting_output(a, 6, device, {moves}, at::kInt, *table), top = fitting_output(a, 7, device, {1}, at::kInt, *table);
+        const at::Tensor workspace = pages_workspace(a, 8, device, B, n_pages, *table);
+        if (!a.ok) return nullptr;
+        const int *tp = pointer<int>(table), *hp = pointer<int>(held);
+        int *ntp = pointer<int>(&new_table), *sp = pointer<int>(&src), *dp = pointer<int>(&dst), *top_p = pointer<int>(&top);
+        void* wp = workspace.data_ptr();
+        const size_t bytes = (size_t)workspace.numel();
+        const int st = without_gil([&] { return lib.cache_compact(tp, hp, ntp, sp, dp, top_p, wp, bytes, B, moves, n_pages, max_pages, stream); });
+        return result(st, a, {4, 5, 6, 7}, {new_table, src, dst, top});
+    });
+}
+
+// (k_pages, v_pages, src, dst, k_scales, v_scales, stream)
+PyObject* cache_copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return native([&]() -> PyObject* {
+        Arguments a(args, n, 7);
+        if (!a.ok) return nullptr;
+        const int device = current_device();
+        PagesArguments c;
+        if (!pages_arguments(a, c, device, 0, 4, 5) || !THPVariable_CheckExact(args[2]) || THPVariable_Unpack(args[2]).dim() != 1) return nullptr;
+        const int64_t pairs = THPVariable_Unpack(args[2]).size(0);
+        if (pairs > 0x7fffffff) return nullptr;
+        const at::Tensor *src = fitting(a, 2, device, {pairs}, at::kInt), *dst = fitting(a, 3, device, {pairs}, at::kInt);
+        void* stream = a.stream(6);
+        if (!a.ok) return nullptr;
+        void *kp = c.k->data_ptr(), *vp = c.v->data_ptr(), *ksp = pointer(c.k_scales), *vsp = pointer(c.v_scales);
+        const int *sp = pointer<int>(src), *dp = pointer<int>(dst);
+        const int st = without_gil([&] { return lib.cache_copy(kp, vp, ksp, vsp, sp, dp, (int)pairs, c.s.H, c.s.d, c.s.N, c.s.B, c.code, stream); });
+        return result(st, a, {0, 1}, {*c.k, *c.v});
+    });
+}
+
 // bind(address of fa_fwd_gqa, fa_fwd_fp8_gqa, fa_fp8_quant_hadamard, fa_bwd_workspace_bytes, fa_bwd_gqa, fa_rope, fa_rope_bwd, fa_cache_write,
-// fa_cache_read, fa_fwd_cache_workspace_bytes, fa_fwd_cache)
+// fa_cache_read, fa_fwd_cache_workspace_bytes, fa_fwd_cache, fa_rope_axes, fa_rope_axes_bwd, fa_cache_pages_workspace_bytes, fa_cache_fork,
+// fa_cache_extend, fa_cache_compact, fa_cache_copy)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    constexpr int kAddresses = 11;
+    constexpr int kAddresses = 18;
     void* p[kAddresses];
     if (n != kAddresses) {
-        PyErr_SetString(PyExc_TypeError, "bind takes eleven addresses");
+        PyErr_SetString(PyExc_TypeError, "bind takes eighteen addresses");
         return nullptr;
     }
     for (int i = 0; i < kAddresses; ++i) {
@@ -560,12 +753,20 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     lib.cache_read = reinterpret_cast<decltype(lib.cache_read)>(p[8]);
     lib.cache_workspace_bytes = reinterpret_cast<decltype(lib.cache_workspace_bytes)>(p[9]);
     lib.fwd_cache = reinterpret_cast<decltype(lib.fwd_cache)>(p[10]);
+    lib.rope_axes = reinterpret_cast<decltype(lib.rope_axes)>(p[11]);
+    lib.rope_axes_bwd = reinterpret_cast<decltype(lib.rope_axes_bwd)>(p[12]);
+    lib.pages_workspace_bytes = reinterpret_cast<decltype(lib.pages_workspace_bytes)>(p[13]);
+    lib.cache_fork = reinterpret_cast<decltype(lib.cache_fork)>(p[14]);
+    lib.cache_extend = reinterpret_cast<decltype(lib.cache_extend)>(p[15]);
+    lib.cache_compact = reinterpret_cast<decltype(lib.cache_compact)>(p[16]);
+    lib.cache_copy = reinterpret_cast<decltype(lib.cache_copy)>(p[17]);
     Py_RETURN_NONE;
 }
 
 #define FA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FA_METHOD(bind), FA_METHOD(fwd), FA_METHOD(fwd_fp8), FA_METHOD(quant), FA_METHOD(bwd), FA_METHOD(rope), FA_METHOD(cache_write),
-                         FA_METHOD(cache_read), FA_METHOD(fwd_cache), {nullptr, nullptr, 0, nullptr}};
+                         FA_METHOD(cache_read), FA_METHOD(fwd_cache), FA_METHOD(rope_axes), FA_METHOD(cache_fork), FA_METHOD(cache_extend),
+                         FA_METHOD(cache_compact), FA_METHOD(cache_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fa_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 // Whether the torch of this process is the one that this file was compiled against; if not, ImportError is set

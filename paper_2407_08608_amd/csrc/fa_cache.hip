@@ -28,7 +28,7 @@ static __device__ __forceinline__ float max_of_lanes(float x) {
 
 // 16 consecutive elements of a row
 template <int DTYPE> struct Elements {
-    static constexpr int ELEM = DTYPE == FA_F32 ? 4 : DTYPE == FA_FP8_E4M3 ? 1 : 2;
+    static constexpr int ELEM = DTYPE == FA_F32 ? 4 : DTYPE == FA_FP8_E4M3 ? 1 : 2, BYTES = 16 * ELEM;
     i32x4 w[ELEM];
     // On the cache's side loads and stores are non-temporal: its pages are many, and the dense tensors are what the launch before
     // or after has in hand.  us, plain / so: 4 prompts of up to 4096 tokens written as codes (16 heads, d = 128) 32.2 / 28.6, 4
@@ -88,6 +88,43 @@ template <int DTYPE> struct Elements {
     }
 };
 
+// 16 elements as e2m1 codes, which the instructions convert from and to values over a scale (to nearest even; to +-6 above 5)
+template <> struct Elements<FA_FP4_E2M1> {
+    static constexpr int BYTES = 8;
+    i32x2 w;
+    template <bool ONCE>
+    __device__ __forceinline__ void load(const char* p) {
+        const i32x2* at = reinterpret_cast<const i32x2*>(p);
+        w = ONCE ? __builtin_nontemporal_load(at) : *at;
+    }
+    template <bool ONCE>
+    __device__ __forceinline__ void store(char* p) const {
+        i32x2* at = reinterpret_cast<i32x2*>(p);
+        if constexpr (ONCE) __builtin_nontemporal_store(w, at);
+        else *at = w;
+    }
+    template <int T>
+    __device__ __forceinline__ void get2(float (&f)[16], float scale) const {
+        const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[T / 4], scale, T % 4);
+        f[2 * T] = y[0];
+        f[2 * T + 1] = y[1];
+    }
+    __device__ __forceinline__ void get(float (&f)[16], float scale) const {
+        static_for<8>([&](auto t) __attribute__((always_inline)) { get2<decltype(t)::value>(f, scale); });
+    }
+    __device__ __forceinline__ void set(const float (&f)[16]) {
+        uint32_t u[2] = {0, 0};
+        static_for<8>([&](auto t) __attribute__((always_inline)) {
+            constexpr int T = decltype(t)::value;
+            u[T / 4] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u[T / 4], f[2 * T], f[2 * T + 1], 1.0f, T % 4);
+        });
+        w = i32x2{(int)u[0], (int)u[1]};
+    }
+};
+
+// The value of a scale of 32 elements, a power of two by its biased exponent; 255 is as good as NaN to the instructions that take it
+static __device__ __forceinline__ float power_of_two(uint32_t biased) { return __builtin_bit_cast(float, biased << 23); }
+
 // The slot of place `at` of sequence b counted over all pages and heads' rows, or -1 where there is none
 static __device__ __forceinline__ long slot_of(const Cache& c, int b, int at, int head) {
     const int entry = (unsigned)at / (unsigned)c.page_size;
@@ -114,6 +151,25 @@ static __device__ __forceinline__ float quantise(float (&f)[16]) {
     return a > 0.f ? a / kE4m3Max : 1.f;
 }
 
+// Values of a half of 32 elements (the other is the neighbouring lane's), in units of their scale, and the scale's biased exponent: of
+// the least power of two s with a <= 7 s, where 7 is what still rounds to the largest code, 6, by no more than half a step
+static __device__ __forceinline__ uint32_t quantise_32(float (&f)[16]) {
+    float a = 0.f;
+    bool nan = false;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        a = fmaxf(a, fabsf(f[t]) < INFINITY ? fabsf(f[t]) : 0.f);
+        nan |= f[t] != f[t];
+    }
+    a = max_dpp<0xB1>(a);
+    const uint32_t any = __builtin_bit_cast(uint32_t, max_dpp<0xB1>(nan ? 1.f : 0.f)), bits = __builtin_bit_cast(uint32_t, a);
+    const uint32_t biased = max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x600000u), 27);  // (no less than 2^-100)
+    const float factor = power_of_two(254 - biased);
+#pragma unroll
+    for (int t = 0; t < 16; ++t) f[t] = fminf(fmaxf(f[t] * factor, -6.f), 6.f);
+    return any ? 255 : biased;
+}
+
 template <int D, int IN, int OUT>
 __global__ void __launch_bounds__(256) fa_cache_write_kernel(Rows k, Rows v, Cache c, const int* counts, unsigned rows, unsigned T) {
     constexpr int LANES = D / 16;
@@ -130,7 +186,7 @@ __global__ void __launch_bounds__(256) fa_cache_write_kernel(Rows k, Rows v, Cac
     if (slot < 0) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        char* to = static_cast<char*>(i ? c.v : c.k) + (slot * D + 16 * lane) * Elements<OUT>::ELEM;
+        char* to = static_cast<char*>(i ? c.v : c.k) + (slot * LANES + lane) * Elements<OUT>::BYTES;
         if constexpr (IN == OUT) {
             x[i].template store<true>(to);
         } else {
@@ -138,7 +194,11 @@ __global__ void __launch_bounds__(256) fa_cache_write_kernel(Rows k, Rows v, Cac
             x[i].get(f);
             if constexpr (OUT == FA_FP8_E4M3) {
                 const float scale = quantise<LANES>(f);
-                if (lane == 0) (i ? c.v_scales : c.k_scales)[slot] = scale;
+                if (lane == 0) static_cast<float*>(i ? c.v_scales : c.k_scales)[slot] = scale;
+            }
+            if constexpr (OUT == FA_FP4_E2M1) {
+                const uint32_t scale = quantise_32(f);
+                if (lane % 2 == 0) static_cast<uint8_t*>(i ? c.v_scales : c.k_scales)[slot * (D / 32) + lane / 2] = (uint8_t)scale;
             }
             Elements<OUT> y;
             y.set(f);
@@ -158,8 +218,8 @@ __global__ void __launch_bounds__(256) fa_cache_read_kernel(Cache c, char* k, ch
     const long slot = slot_of(c, b, n, h);  // (looked up before the length is known)
     if (n >= len || slot < 0) return;
     Elements<IN> x[2];
-    x[0].template load<true>(static_cast<const char*>(c.k) + (slot * D + 16 * lane) * Elements<IN>::ELEM);
-    x[1].template load<true>(static_cast<const char*>(c.v) + (slot * D + 16 * lane) * Elements<IN>::ELEM);
+    x[0].template load<true>(static_cast<const char*>(c.k) + (slot * LANES + lane) * Elements<IN>::BYTES);
+    x[1].template load<true>(static_cast<const char*>(c.v) + (slot * LANES + lane) * Elements<IN>::BYTES);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         char* to = (i ? v : k) + ((long)row * D + 16 * lane) * Elements<OUT>::ELEM;
@@ -167,9 +227,11 @@ __global__ void __launch_bounds__(256) fa_cache_read_kernel(Cache c, char* k, ch
             x[i].template store<false>(to);
         } else {
             float f[16];
-            x[i].get(f);
+            if constexpr (IN == FA_FP4_E2M1)
+                x[i].get(f, power_of_two(static_cast<const uint8_t*>(i ? c.v_scales : c.k_scales)[slot * (D / 32) + lane / 2]));
+            else x[i].get(f);
             if constexpr (IN == FA_FP8_E4M3) {
-                const float scale = (i ? c.v_scales : c.k_scales)[slot];
+                const float scale = static_cast<const float*>(i ? c.v_scales : c.k_scales)[slot];
 #pragma unroll
                 for (int t = 0; t < 16; ++t) f[t] *= scale;
             }
@@ -186,6 +248,7 @@ static int with_types(int d, int dense, int cache, F&& f) {
     auto by_cache = [&](auto D, auto dense_type) {
         constexpr int X = decltype(dense_type)::value;
         if (cache == FA_FP8_E4M3) return f(D, dense_type, std::integral_constant<int, FA_FP8_E4M3>{});
+        if (cache == FA_FP4_E2M1) return f(D, dense_type, std::integral_constant<int, FA_FP4_E2M1>{});
         if constexpr (X != FA_F16)
             if (cache == FA_BF16) return f(D, dense_type, std::integral_constant<int, FA_BF16>{});
         if constexpr (X != FA_BF16)

@@ -23,6 +23,10 @@
 //   - e4m3: codes become 16-bit operands in registers (exact): K in the type of Q, with the key's scale on the score; V in
 //     bf16, with P~ = p v scale as two bf16 numbers, a rounded value and what that leaves out.  Their range is that of the scales, so
 //     no weight depends on a scale of another key, seen or not, and sixteen bits of each reach the product.
+//   - e2m1: a wave brings its tiles' codes and scales to registers while it works on the tile before, and puts the values, which are bf16
+//     numbers whatever their scales, into the LDS as a tile of a bf16 cache, which they are from there on.  So each is converted once for
+//     all rows, transposing reads are the 16-bit ones, and no scale is left that a score or a weight would have to bear.  Q in fp16
+//     goes to the scores as two bf16 numbers, which is exact, and P as two as with e4m3.
 //   - 16 columns where a group has no more rows (v_mfma_16x16x32 instead of 32x32x16): half the registers, matrix and vector
 //     instructions for a tile.
 #include "fa_device.h"
@@ -123,6 +127,11 @@ static __device__ __forceinline__ i32x4 from_codes(int lo, int hi) {
         w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
     }
     return w;
+}
+
+// A code (its low four bits) over its scale's biased exponent
+static __device__ __forceinline__ float e2m1_value(uint32_t code, uint32_t biased) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, __builtin_bit_cast(float, biased << 23), 0)[0];
 }
 
 // The two shapes of the matrix products, by the columns (queries) of a tile.  Lane (col, part): col = lane % COLS.
@@ -303,6 +312,74 @@ struct CacheTile {
     }
 };
 
+// A row number of lane i's in scalar registers; negative: none.  (Two words: there is no scalar comparison of 64 bits.)
+struct UniformRow {
+    int lo, hi;
+    UniformRow() = default;
+    __device__ __forceinline__ UniformRow(long v, int i) : lo(__builtin_amdgcn_readlane((int)v, i)), hi(__builtin_amdgcn_readlane((int)(v >> 32), i)) {
+        asm volatile("" : "+s"(lo), "+s"(hi));  // (or the two are compared as one again)
+    }
+    __device__ __forceinline__ int none() const { return hi >> 31; }  // all bits set, or none
+    __device__ __forceinline__ long index() const { return (long)((uint64_t)(uint32_t)(lo & ~none()) | (uint64_t)(uint32_t)(hi & ~none()) << 32); }
+};
+
+// What the cache holds: 16-bit words, e4m3 codes, e2m1 codes
+enum Held { kWords, kCodes8, kCodes4 };
+
+// A wave's tile of 32 rows of e2m1 codes, or with HALF 16 of them, on its way from the pages to the LDS.  Lane l has words i 64 + l of the
+// codes in a row, each eight elements, which are 16 bytes of the tile in the LDS, side by side; and word l of the scales, four bytes: the
+// one of code word w is byte w / 4 % 4 of word w / 16.
+template <int D, bool HALF>
+struct RawTile {
+    static constexpr int ROWS = HALF ? 16 : 32, ROWB = D / 2, WPR = D / 8, N = ROWS * WPR / 64, SCALES = 4 * N;
+    int code[N], scale;
+
+    struct Run {  // 16 rows, or as many as there are
+        const void* codes;
+        int bytes;
+    };
+    // runs: rows 0 .. 15 and 16 .. 31; row: their number, 0 for no page (whose scales are there, and not looked at)
+    template <int RUNS>
+    __device__ __forceinline__ void request(const void* scales, const Run (&runs)[RUNS], const UniformRow (&row)[RUNS], int lane) {
+        constexpr int EACH = SCALES / RUNS;
+        static_for<N>([&](auto n) __attribute__((always_inline)) {
+            constexpr int i = decltype(n)::value, h = i / (N / RUNS);
+            code[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(make_buffer(runs[h].codes, runs[h].bytes), lane * 4 + (i - h * (N / RUNS)) * 256, 0, kStreamed);
+        });
+        const int w = lane & (SCALES - 1);
+        long at = row[0].index();
+        if constexpr (RUNS == 2) {
+            long upper = row[1].index();
+            asm volatile("" : "+v"(at), "+v"(upper));
+            at = w >= EACH ? upper : at;
+        }
+        scale = *reinterpret_cast<const int*>(static_cast<const char*>(scales) + at * (D / 32) + 4 * (w & (EACH - 1)));
+    }
+    // `to`: the lane's place for word l of the first row; swizzle(r): what further rows change in it.  there, bad: rows from `there` on, and
+    // those of halves on no page, get a scale that makes zeros of the zeros that arrived
+    template <typename Swizzle>
+    __device__ __forceinline__ void put(uint32_t to, uint32_t offset, int lane, int there, int bad, Swizzle&& swizzle) const {
+        typedef i32x4 __attribute__((address_space(3))) * lds_vec_ptr;
+        const bool all = there >= ROWS && bad == 0;
+        static_for<N>([&](auto n) __attribute__((always_inline)) {
+            constexpr int i = decltype(n)::value, r0 = i * 64 / WPR;
+            const uint32_t word = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (4 * i + (lane >> 4)), scale);
+            uint32_t biased = word >> (2 * (lane & 12)) & 255;  // (byte lane / 4 % 4)
+            if (!all) {
+                const int r = r0 + lane / WPR;
+                if (r >= there || (bad >> (r >> 4) & 1)) biased = 0;
+            }
+            const float s = __builtin_bit_cast(float, biased << 23);
+            i32x4 y;
+            y[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)code[i], s, 0));
+            y[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)code[i], s, 1));
+            y[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)code[i], s, 2));
+            y[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)code[i], s, 3));
+            *(lds_vec_ptr)(uintptr_t)((to ^ (uint32_t)(swizzle(r0) << 4)) + (offset + i * 1024)) = y;
+        });
+    }
+};
+
 // Asynchronous copy of 4 bytes per lane from an address per lane to lds_base + 4 lane
 static __device__ __forceinline__ void global_to_lds_4B(const float* p, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
@@ -320,23 +397,13 @@ static __device__ __forceinline__ void wait_vmcnt() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// A row number of lane i's in scalar registers; negative: none.  (Two words: there is no scalar comparison of 64 bits.)
-struct UniformRow {
-    int lo, hi;
-    UniformRow() = default;
-    __device__ __forceinline__ UniformRow(long v, int i) : lo(__builtin_amdgcn_readlane((int)v, i)), hi(__builtin_amdgcn_readlane((int)(v >> 32), i)) {
-        asm volatile("" : "+s"(lo), "+s"(hi));  // (or the two are compared as one again)
-    }
-    __device__ __forceinline__ int none() const { return hi >> 31; }  // all bits set, or none
-    __device__ __forceinline__ long index() const { return (long)((uint64_t)(uint32_t)(lo & ~none()) | (uint64_t)(uint32_t)(hi & ~none()) << 32); }
-};
-
 // FORM: the waves of a workgroup either share its rows and divide the keys (kDivideKeys), or they have RT tiles of rows each and
 // share the keys, which they stage together (kShareKeys).
 enum Form { kDivideKeys, kShareKeys };
-template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG, int FORM>
+template <typename Tag, int D, int HELD, int COLS, int RT, int NW, int STG, int FORM>
 struct CachedShape {
-    using Tile = CacheTile<Tag, D, CODES, COLS>;
+    static constexpr bool CODES = HELD == kCodes8;
+    using Tile = CacheTile<std::conditional_t<HELD == kCodes4, bf16_tag, Tag>, D, CODES, COLS>;
     static constexpr bool SHARED = FORM == kShareKeys;
     static constexpr int ROWS = COLS * RT * (SHARED ? NW : 1);  // of a workgroup
     static constexpr int STEP = 32 * NW;                        // keys of a step
@@ -347,14 +414,16 @@ struct CachedShape {
     static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
     // workgroups (of four waves) to a CU, by registers
     static constexpr int WAVES = SHARED ? (D == 64 ? 3 : D == 128 ? 2 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
+    static_assert(LDS <= 163840);
     static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;
 };
 
-template <typename Tag, int D, bool CODES, int COLS, int RT, int NW, int STG, int FORM>
-__global__ void __launch_bounds__(NW * 64, (CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>::WAVES))
+template <typename Tag, int D, int HELD, int COLS, int RT, int NW, int STG, int FORM>
+__global__ void __launch_bounds__(NW * 64, (CachedShape<Tag, D, HELD, COLS, RT, NW, STG, FORM>::WAVES))
 fa_fwd_cache_kernel(CachedArgs a) {
-    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>;
-    constexpr bool SHARED = Shape::SHARED;
+    using Shape = CachedShape<Tag, D, HELD, COLS, RT, NW, STG, FORM>;
+    constexpr bool SHARED = Shape::SHARED, CODES = HELD == kCodes8, FOUR = HELD == kCodes4;
+    constexpr bool Q_IN_TWO = FOUR && std::is_same_v<Tag, f16_tag>;
     constexpr int KW = SHARED ? 1 : NW, RW = SHARED ? NW : 1;  // waves that divide keys, that have rows of their own
     using Tile = typename Shape::Tile;
     using M = typename Tile::M;
@@ -368,7 +437,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // With codes always: one bf16 number would be eight times as coarse as the fp16 number that a factor common to all keys allows, and
     // no common factor is right where a key of a large scale weighs little, or nothing (8 trees of 32 tokens, 8 heads: 53.0 us, with
     // fp16 and such a factor 51.3; 64 x 500 to 4096 keys, T = 1, d = 64: 26.1 and 27.8).
-    constexpr bool TWO_PARTS = COLS == 16 || CODES;
+    constexpr bool TWO_PARTS = COLS == 16 || CODES || Q_IN_TWO;
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -501,7 +570,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
             row = lane & 16 ? upper : row;
             const int there = key1 - (key0 + 32 * (kw + KW * i));
             const long at = (lane & 31) >= there ? 0 : row + (lane & 15);
-            global_to_lds_4B((lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + st * Shape::STAGE_B + 2 * Tile::TILE_B);
+            global_to_lds_4B(static_cast<const float*>(lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + st * Shape::STAGE_B + 2 * Tile::TILE_B);
         }
     };
     auto request_v = [&](int i, auto stage) __attribute__((always_inline)) {
@@ -530,11 +599,53 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 asm volatile("" : "+v"(at_row), "+v"(upper));
                 at_row = lane & 16 ? upper : at_row;
                 const long at = (lane & 31) >= there ? 0 : at_row + (lane & 15);
-                global_to_lds_4B((lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + offset + 2 * Tile::TILE_B);
+                global_to_lds_4B(static_cast<const float*>(lane & 32 ? a.c.v_scales : a.c.k_scales) + at, tile.base + offset + 2 * Tile::TILE_B);
             }
     };
+    // e2m1: tile i on its way in registers, and what of it is on no page; kDivideKeys: K and V of the wave's own, kShareKeys: the wave's quarter
+    // of the tile that all share (as above)
+    using Raw = RawTile<D, SHARED>;
+    Raw raw[SHARED ? 1 : 2];
+    int raw_bad = 0;
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        if constexpr (!FOUR) return;
+        else {
+        if ((i & 63) == 0 && i > 0) look_up(i);
+        const UniformRow lo(row_lo, i & 63), hi(row_hi, i & 63);
+        raw_bad = (lo.none() & 1) | (hi.none() & 2);
+        auto resource = [&](const void* pages, const UniformRow& row, int h) __attribute__((always_inline)) {
+            int n = max(key1 - (key0 + 32 * (kw + KW * i)) - 16 * h, 0);
+            asm volatile("" : "+s"(n));
+            n = min(n, 16) & ~row.none();
+            return typename Raw::Run{static_cast<const char*>(pages) + row.index() * Raw::ROWB, n * Raw::ROWB};
+        };
+        if constexpr (SHARED) {
+            const UniformRow row[1] = {wave & 1 ? hi : lo};
+            const typename Raw::Run run[1] = {resource(wave & 2 ? a.c.v : a.c.k, row[0], wave & 1)};
+            raw[0].request(wave & 2 ? a.c.v_scales : a.c.k_scales, run, row, lane);
+        } else {
+            const UniformRow row[2] = {lo, hi};
+            const typename Raw::Run k[2] = {resource(a.c.k, lo, 0), resource(a.c.k, hi, 1)}, v[2] = {resource(a.c.v, lo, 0), resource(a.c.v, hi, 1)};
+            raw[0].request(a.c.k_scales, k, row, lane);
+            raw[SHARED ? 0 : 1].request(a.c.v_scales, v, row, lane);
+        }
+        }
+    };
+    // puts what has been fetched of tile i where tiles are read, at `offset`
+    auto put = [&](int i, uint32_t offset) __attribute__((always_inline)) {
+        if constexpr (FOUR) {
+        const int there = key1 - (key0 + 32 * (kw + KW * i));
+        auto swizzle = [](int r) __attribute__((always_inline)) { return Tile::swizzle(r); };
+        if constexpr (SHARED) {
+            raw[0].put(tile.base + src_shared, offset + (wave >> 1) * Tile::TILE_B + (wave & 1) * (Tile::TILE_B / 2), lane, there - 16 * (wave & 1), raw_bad >> (wave & 1), swizzle);
+        } else {
+            raw[0].put(tile.base + tile.src0, offset, lane, there, raw_bad, swizzle);
+            raw[SHARED ? 0 : 1].put(tile.base + tile.src0, offset + Tile::TILE_B, lane, there, raw_bad, swizzle);
+        }
+        }
+    };
     int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
-    i32x4 qreg[RT][QS];
+    i32x4 qreg[RT][QS], qrest[RT][Q_IN_TWO ? QS : 1];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int row = min(((rg * RW + rw) * RT + x) * COLS + col, max(n_rows - 1, 0)), g = row / per;
@@ -544,6 +655,16 @@ fa_fwd_cache_kernel(CachedArgs a) {
         for (int u = 0; u < QS; ++u) {
             const int at = CODES ? 16 * M::PARTS * (u / 2) + 16 * part + 8 * (u % 2) : 8 * M::PARTS * u + 8 * part;
             qreg[x][u] = *reinterpret_cast<const i32x4*>(q + at);
+            if constexpr (Q_IN_TWO) {
+                const i32x4 w = qreg[x][u];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float lo = E::to_float((uint16_t)w[e]), hi = E::to_float((uint16_t)((uint32_t)w[e] >> 16));
+                    const int y = PE::pack2(lo, hi);
+                    qreg[x][u][e] = y;
+                    qrest[x][u][e] = PE::pack2(lo - PE::to_float((uint16_t)y), hi - PE::to_float((uint16_t)((uint32_t)y >> 16)));
+                }
+            }
         }
     }
     // Q is on its way while the table is read, and there before the first request: the compiler, which does not see the requests,
@@ -552,9 +673,19 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
-        for (int u = 0; u < QS; ++u) asm volatile("" : "+v"(qreg[x][u]));
+        for (int u = 0; u < QS; ++u) {
+            asm volatile("" : "+v"(qreg[x][u]));
+            if constexpr (Q_IN_TWO) asm volatile("" : "+v"(qrest[x][u]));
+        }
     if (mine > 0) {
-        if constexpr (SHARED) {
+        if constexpr (FOUR) {
+            fetch(0);
+            if constexpr (SHARED) {
+                put(0, 0);
+                pending = raw_bad;
+                fetch(1);
+            }
+        } else if constexpr (SHARED) {
 #pragma unroll
             for (int i = 0; i < STG - 1; ++i) request_shared(i, i * Shape::STAGE_B, i);
         } else {
@@ -624,7 +755,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
                             for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(hi, qreg[x][2 * k + 1], y[x][kt]);
                         } else {
 #pragma unroll
-                            for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(w, qreg[x][k], y[x][kt]);
+                            for (int x = 0; x < RT; ++x) {
+                                y[x][kt] = M::mma(w, qreg[x][k], y[x][kt]);
+                                if constexpr (Q_IN_TWO) y[x][kt] = M::mma(w, qrest[x][k], y[x][kt]);
+                            }
                         }
                     });
                 });
@@ -749,7 +883,33 @@ fa_fwd_cache_kernel(CachedArgs a) {
             });
             after_products();
     };
-    if constexpr (SHARED) {
+    if constexpr (FOUR && SHARED) {
+        // Tile i + 1 goes where tile i - 1 was, which all waves have left when they meet in tile i
+        for (int i0 = 0; i0 < mine; i0 += STG)
+            static_for<STG>([&](auto stage) __attribute__((always_inline)) {
+                constexpr int st = decltype(stage)::value;
+                static_assert(STG == 2);
+                const int i = i0 + st;
+                if (i >= mine) return;
+                barrier();
+                put(i + 1, (st ^ 1) * Shape::STAGE_B);
+                const int bad = pending;
+                pending = raw_bad;
+                fetch(i + 2);
+                work(tile, std::integral_constant<int, st * Shape::STAGE_B>{}, key0 + 32 * i, bad, [] {}, [] {}, [] {});
+            });
+    } else if constexpr (FOUR) {
+        static_assert(STG == 1);
+        for (int i = 0; i < mine; ++i) {
+            // (a wave's LDS instructions are done in order: what it reads of the tile before comes first, what it puts here ahead of what it reads)
+            asm volatile("" ::: "memory");
+            put(i, 0);
+            asm volatile("" ::: "memory");
+            const int bad = raw_bad;
+            fetch(i + 1);
+            work(tile, std::integral_constant<int, 0>{}, key0 + 32 * (kw + KW * i), bad, [] {}, [] {}, [] {});
+        }
+    } else if constexpr (SHARED) {
         // Tile i + STG - 1 goes where tile i - 1 was, which all waves have left when they meet in tile i
         for (int i0 = 0; i0 < mine; i0 += STG)
             static_for<STG>([&](auto stage) __attribute__((always_inline)) {
@@ -845,10 +1005,12 @@ fa_fwd_cache_kernel(CachedArgs a) {
                         const bool sees = u < 0 ? true : a.tree ? a.tree[((long)(a.tree_batches == 1 ? 0 : b) * a.T + tok) * words + (u >> 5)] >> (u & 31) & 1 : u <= tok;
                         const int page = a.c.block_table[(long)b * a.c.max_pages + entry];
                         if (!sees || page < 0 || page >= a.c.n_pages) continue;
-                        const long at = (((long)page * H_kv + kvh) * a.c.page_size + (place - entry * a.c.page_size)) * D + c0 + cc;
+                        const long slot = ((long)page * H_kv + kvh) * a.c.page_size + (place - entry * a.c.page_size), at = slot * D + c0 + cc;
                         for (int e = 0; e < 8; ++e) {
                             float v;
                             if constexpr (CODES) v = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(a.c.v)[at + e], 0);
+                            else if constexpr (FOUR)
+                                v = e2m1_value(static_cast<const uint8_t*>(a.c.v)[(at + e) >> 1] >> (4 * (e & 1)), static_cast<const uint8_t*>(a.c.v_scales)[(at + e) >> 5]);
                             else v = E::to_float(static_cast<const uint16_t*>(a.c.v)[at + e]);
                             if (!(fabsf(v) < INFINITY))
 #pragma unroll
@@ -998,35 +1160,41 @@ static bool whole_sequences(double workgroups, int max_len) {
 // Eight waves instead of four halve the chain of a sequence that a workgroup has for itself, where its keys are small enough for two
 // such workgroups' worth of LDS to be worth it: us, four / eight, T = 1, 8 heads: d = 64 1024 9.7 / 8.3; codes d = 64 768 9.9 / 8.1,
 // d = 128 768 10.5 / 9.3, d = 256 512 12.7 / 11.6; bf16 d = 128 768 11.2 / 10.3 but 2048 22.2 / 21.7, and 300 7.5 / 7.7.
-template <int D_, bool CODES_, int COLS_, int RT_, int NW_, int FORM_>
+template <int D_, int HELD_, int COLS_, int RT_, int NW_, int FORM_>
 struct CachedForm {
-    static constexpr int D = D_, COLS = COLS_, RT = RT_, NW = NW_, FORM = FORM_, STG = FORM == kShareKeys ? 3 : 1;
-    static constexpr bool CODES = CODES_;
+    static constexpr int D = D_, HELD = HELD_, COLS = COLS_, RT = RT_, NW = NW_, FORM = FORM_, STG = FORM != kShareKeys ? 1 : HELD == kCodes4 ? 2 : 3;
+    static constexpr bool CODES = HELD != kWords;
     template <typename Tag>
-    using Shape = CachedShape<Tag, D, CODES, COLS, RT, NW, STG, FORM>;
+    using Shape = CachedShape<Tag, D, HELD, COLS, RT, NW, STG, FORM>;
 };
 template <typename F>
-static auto with_form(int B, int H_kv, int rows, int d, int max_len, bool codes, F&& f) {
-    auto by_rows = [&](auto D, auto c) {
-        constexpr int d_ = decltype(D)::value;
-        constexpr bool c_ = decltype(c)::value;
+static auto with_form(int B, int H_kv, int rows, int d, int max_len, int cache_dtype, F&& f) {
+    auto by_rows = [&](auto D, auto held) {
+        constexpr int d_ = decltype(D)::value, h_ = decltype(held)::value;
+        constexpr bool c_ = h_ != kWords;
         if (rows <= 16) {
-            if constexpr (d_ == 64 || c_) {
-                using Eight = CachedForm<d_, c_, 16, 1, 8, kDivideKeys>;
+            if constexpr (d_ == 64 || h_ == kCodes8 || (h_ == kCodes4 && d_ == 128)) {  // (what of eight waves fits the LDS)
+                using Eight = CachedForm<d_, h_, 16, 1, 8, kDivideKeys>;
                 if ((double)B * H_kv <= (c_ && d_ == 128 ? 256 : 128) && max_len > 256 && whole_sequences<Eight>((double)B * H_kv, max_len)) return f(Eight{});
             }
-            return f(CachedForm<d_, c_, 16, 1, 4, kDivideKeys>{});
+            return f(CachedForm<d_, h_, 16, 1, 4, kDivideKeys>{});
         }
-        if (rows > 64) return f(CachedForm<d_, c_, 32, 1, 4, kShareKeys>{});
+        if (rows > 64) return f(CachedForm<d_, h_, 32, 1, 4, kShareKeys>{});
         if constexpr (d_ < 256)
-            if (rows > 32) return f(CachedForm<d_, c_, 32, 2, 4, kDivideKeys>{});
-        return f(CachedForm<d_, c_, 32, 1, 4, kDivideKeys>{});
+            if (rows > 32) return f(CachedForm<d_, h_, 32, 2, 4, kDivideKeys>{});
+        return f(CachedForm<d_, h_, 32, 1, 4, kDivideKeys>{});
     };
-    auto by_codes = [&](auto D) { return codes ? by_rows(D, std::true_type{}) : by_rows(D, std::false_type{}); };
+    auto by_held = [&](auto D) {
+        switch (cache_dtype) {
+            case FA_FP8_E4M3: return by_rows(D, std::integral_constant<int, kCodes8>{});
+            case FA_FP4_E2M1: return by_rows(D, std::integral_constant<int, kCodes4>{});
+            default: return by_rows(D, std::integral_constant<int, kWords>{});
+        }
+    };
     switch (d) {
-        case 64: return by_codes(std::integral_constant<int, 64>{});
-        case 128: return by_codes(std::integral_constant<int, 128>{});
-        default: return by_codes(std::integral_constant<int, 256>{});
+        case 64: return by_held(std::integral_constant<int, 64>{});
+        case 128: return by_held(std::integral_constant<int, 128>{});
+        default: return by_held(std::integral_constant<int, 256>{});
     }
 }
 
@@ -1064,7 +1232,7 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
     }
     const double total = (double)(div.teams != 0 ? div.teams : (double)a.B * a.c.H_kv) * a.row_groups;
     if (total * 64 * NW >= 4294967296.0) return FA_ERR_LAUNCH;
-    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, Form::CODES, Form::COLS, Form::RT, NW, Form::STG, Form::FORM>), dim3((unsigned)total), dim3(NW * 64), Shape::LDS, stream, a);
+    hipLaunchKernelGGL((fa_fwd_cache_kernel<Tag, D, Form::HELD, Form::COLS, Form::RT, NW, Form::STG, Form::FORM>), dim3((unsigned)total), dim3(NW * 64), Shape::LDS, stream, a);
     if (hipGetLastError() != hipSuccess) return FA_ERR_LAUNCH;
     if (div.teams != 0) {
         const long rows = (long)a.B * a.H * a.T;
@@ -1079,14 +1247,14 @@ static int launch_cached(CachedArgs a, void* workspace, int max_len, hipStream_t
 }  // namespace
 
 size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype) {
-    return with_form(B, H_kv, H / H_kv * T, d, max_len, cache_dtype == FA_FP8_E4M3,
+    return with_form(B, H_kv, H / H_kv * T, d, max_len, cache_dtype,
                      [&](auto form) { return CachedDivision(form, B, H, H_kv, T, max_len).bytes(d); });
 }
 
 int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
                      void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream) {
     const CachedArgs a = {q, o, cache, counts, tree, lse, nullptr, nullptr, nullptr, B, H, T, tree_batches, 1, 0, scale};
-    return with_form(B, cache.H_kv, H / cache.H_kv * T, d, max_len, cache.dtype == FA_FP8_E4M3, [&](auto form) {
+    return with_form(B, cache.H_kv, H / cache.H_kv * T, d, max_len, cache.dtype, [&](auto form) {
         using Form = decltype(form);
         return dtype == FA_BF16 ? launch_cached<bf16_tag, Form>(a, workspace, max_len, stream) : launch_cached<f16_tag, Form>(a, workspace, max_len, stream);
     });

@@ -352,11 +352,16 @@ struct Rows {
 int launch_rope(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
                 int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved, bool transposed, int dtype,
                 hipStream_t stream);
+// axis: which of the `axes` arrays of positions each pair goes by
+int launch_rope_axes(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
+                     const int* axis, int axes, int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved,
+                     bool transposed, int dtype, hipStream_t stream);
 
-// A paged cache (include/fa_mi355.h): pages [n_pages][H_kv][page_size][d], scales without the last dimension, NULL for 16 bits
+// A paged cache (include/fa_mi355.h): pages [n_pages][H_kv][page_size][d], and scales: a float for each row of e4m3 codes, a byte for
+// each 32 elements of a row of e2m1 codes, NULL for 16 bits
 struct Cache {
     void *k, *v;
-    float *k_scales, *v_scales;
+    void *k_scales, *v_scales;
     const int *block_table, *lens;
     int H_kv, page_size, n_pages, max_pages, dtype;
 };
@@ -368,6 +373,15 @@ int launch_cache_read(const Cache& cache, void* k, void* v, int B, int N, int d,
 size_t fwd_cache_workspace_bytes(int B, int H, int H_kv, int T, int d, int max_len, int cache_dtype);
 int launch_fwd_cache(const Rows& q, const Cache& cache, const int* counts, const int* tree, int tree_batches, const Rows& o, float* lse,
                      void* workspace, int B, int H, int T, int d, int max_len, float scale, int dtype, hipStream_t stream);
+
+size_t cache_pages_workspace_bytes(int B, int n_pages);
+int launch_cache_fork(const int* block_table, const int* lens, const int* parents, const int* held, int* new_table, int* new_lens, int* src,
+                      int* dst, int* missing, void* workspace, int B, int B_new, int page_size, int n_pages, int max_pages, hipStream_t stream);
+int launch_cache_extend(int* block_table, const int* lens, const int* counts, const int* held, int* missing, void* workspace, int B, int T,
+                        int page_size, int n_pages, int max_pages, hipStream_t stream);
+int launch_cache_compact(const int* block_table, const int* held, int* new_table, int* src, int* dst, int* top, void* workspace, int B,
+                         int moves, int n_pages, int max_pages, hipStream_t stream);
+int launch_cache_copy(const Cache& cache, const int* src, const int* dst, int n, int d, hipStream_t stream);
 
 int launch_probe_mfma(const void* operands, size_t operand_bytes, float* sink, int iters, bool fp8, hipStream_t stream);
 double probe_mfma_flops(int iters, bool fp8);

@@ -18,7 +18,9 @@ namespace fa {
 struct RopeArgs {
     Rows x[2], y[2];  // Q and K
     const double* inv_freq;
-    const int* positions;  // [B][N] or NULL
+    const int* positions;  // [B][N] or NULL; with several axes [axes][B][N]
+    const int* axis;       // [rot_dim / 2] with several axes
+    int axes;
     int heads_q, heads, B, N, rot_dim, heads_per_group;
     float amplitude, sign;
 };
@@ -62,7 +64,7 @@ template <int DTYPE> struct RowChunk {  // 8 elements as floats
     }
 };
 
-template <int D, int DTYPE, bool INTERLEAVED, bool ONCE>
+template <int D, int DTYPE, bool INTERLEAVED, bool ONCE, bool AXES>
 __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
     constexpr int TPR = D / 16, ELEM = RowChunk<DTYPE>::ELEM;  // threads per token
     const unsigned token = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
@@ -73,10 +75,15 @@ __global__ void __launch_bounds__(256) fa_rope_kernel(RopeArgs a) {
     const int c0 = turned ? unit : 2 * unit, c1 = turned ? unit + pairs : 2 * unit + 1;
     float co[8], si[8];
     if (turned) {
-        const double turns = 0.15915494309189533577 * (double)(a.positions ? a.positions[token] : n);  // of frequency 1
+        double turns = 0.0;  // of frequency 1
+        if constexpr (!AXES) turns = 0.15915494309189533577 * (double)(a.positions ? a.positions[token] : n);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             const int i = INTERLEAVED ? (t < 4 ? 4 * c0 + t : 4 * c1 + t - 4) : 8 * c0 + t;
+            if constexpr (AXES) {  // (an axis that there is not turns nothing)
+                const int axis = a.axis[i];
+                turns = (unsigned)axis < (unsigned)a.axes ? 0.15915494309189533577 * (double)a.positions[(long)axis * a.B * a.N + token] : 0.0;
+            }
             double phi = turns * a.inv_freq[i];
             phi -= __builtin_rint(phi);
             float s, c;
@@ -137,15 +144,19 @@ template <int D, int DTYPE>
 static int launch_rope_d(const RopeArgs& a, int interleaved, const dim3& grid, hipStream_t stream) {
     const bool once = (double)a.B * a.heads * a.N * D * RowChunk<DTYPE>::ELEM > kReadOnce;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
-    if (interleaved) once ? go(fa_rope_kernel<D, DTYPE, true, true>) : go(fa_rope_kernel<D, DTYPE, true, false>);
-    else once ? go(fa_rope_kernel<D, DTYPE, false, true>) : go(fa_rope_kernel<D, DTYPE, false, false>);
+    auto by_axes = [&](auto axes) {
+        constexpr bool A = decltype(axes)::value;
+        if (interleaved) once ? go(fa_rope_kernel<D, DTYPE, true, true, A>) : go(fa_rope_kernel<D, DTYPE, true, false, A>);
+        else once ? go(fa_rope_kernel<D, DTYPE, false, true, A>) : go(fa_rope_kernel<D, DTYPE, false, false, A>);
+    };
+    a.axis ? by_axes(std::true_type{}) : by_axes(std::false_type{});
     return hipGetLastError() == hipSuccess ? FA_OK : FA_ERR_LAUNCH;
 }
 
-int launch_rope(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
-                int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved, bool transposed, int dtype,
-                hipStream_t stream) {
-    RopeArgs a = {{q, k}, {q_out, k_out}, inv_freq, positions, H, H + H_kv, B, N, rot_dim, 0, amplitude, transposed ? -1.f : 1.f};
+int launch_rope_axes(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
+                     const int* axis, int axes, int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved,
+                     bool transposed, int dtype, hipStream_t stream) {
+    RopeArgs a = {{q, k}, {q_out, k_out}, inv_freq, positions, axis, axes, H, H + H_kv, B, N, rot_dim, 0, amplitude, transposed ? -1.f : 1.f};
     const long per = 256 / (d / 16), tiles = ((long)B * N + per - 1) / per;
     a.heads_per_group = (int)((tiles * a.heads + 2047) / 2048);
     if (a.heads_per_group > 16) a.heads_per_group = 16;
@@ -163,6 +174,13 @@ int launch_rope(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_o
         default: FA_ROPE_D(256)
     }
 #undef FA_ROPE_D
+}
+
+int launch_rope(const Rows& q, const Rows& k, const Rows& q_out, const Rows& k_out, const double* inv_freq, const int* positions,
+                int B, int H, int H_kv, int N, int d, int rot_dim, float amplitude, int interleaved, bool transposed, int dtype,
+                hipStream_t stream) {
+    return launch_rope_axes(q, k, q_out, k_out, inv_freq, positions, nullptr, 0, B, H, H_kv, N, d, rot_dim, amplitude, interleaved, transposed,
+                            dtype, stream);
 }
 
 }  // namespace fa
