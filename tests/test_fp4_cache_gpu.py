@@ -3,7 +3,7 @@ element.  Whatever a row must not see holds NaN scales over random codes.
 
 The bound of a row, with s_j its scores, w_j = p_j / sum p its weights, eps half a step of a type (bf16 2^-8, fp16 2^-11), and every cached
 value a bf16 number as it is:
-  scores    products are exact in fp32, d of them are summed, or 2 d where fp16 Q goes in as two numbers:
+  scores    products are exact in fp32 and d of them are summed; with fp16 Q K is in units, powers of two, of its row's largest scale:
             e_s = (2 d + 4) 2^-24 scale max_j sum |q k_j|
   weights   the argument of the exponential, in units of log 2, is rounded at |s| and |m|: 2^-22 max |s|; the exponential itself 2^-21;
             numerator and sum both: e_w = 2 (e_s + 2^-22 max |s| + 2^-21)
