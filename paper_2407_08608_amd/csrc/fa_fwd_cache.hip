@@ -292,9 +292,10 @@ struct CacheTile {
             return (full >> 15) * 0xFFFFu;
         }
     }
+    static constexpr int LOOKED_AT = NATURAL ? 2 : NI;  // at a time (the registers of all would be missing in the loop)
     __device__ __forceinline__ bool not_finite(uint32_t offset, int lane) const {
         uint32_t any = 0;
-#pragma unroll
+#pragma unroll LOOKED_AT
         for (int i = 0; i < NI; ++i) {
             const i32x4 w = lds_load_16B(base + offset + i * 1024 + lane * 16);
             any |= odd_ones(w[0]) | odd_ones(w[1]) | odd_ones(w[2]) | odd_ones(w[3]);
@@ -303,7 +304,7 @@ struct CacheTile {
     }
     __device__ __forceinline__ void clear_not_finite(uint32_t offset, int lane) const {
         typedef i32x4 __attribute__((address_space(3))) * lds_vec_ptr;
-#pragma unroll
+#pragma unroll LOOKED_AT
         for (int i = 0; i < NI; ++i) {
             const uint32_t at = base + offset + i * 1024 + lane * 16;
             i32x4 w = lds_load_16B(at);
@@ -436,7 +437,7 @@ struct CachedShape {
     using Tile = CacheTile<std::conditional_t<HELD == kCodes4, bf16_tag, Tag>, D, CODES, COLS, HELD == kCodes4>;
     static constexpr bool SHARED = FORM == kShareKeys;
     static constexpr int ROWS = COLS * RT * (SHARED ? NW : 1);  // of a workgroup
-    static constexpr int STEP = 32 * NW;                        // keys of a step
+    static constexpr int STEP = SHARED && HELD == kCodes4 ? 64 : 32 * NW;  // keys of a step
     static constexpr int SCALE_B = HELD == kWords ? 0 : 256;    // of a tile: 32 scales of K, 32 of V; e2m1: 32 units of K
     static constexpr int STAGE_B = (HELD == kCodes4 && !SHARED ? 1 : 2) * Tile::TILE_B + SCALE_B, STAGES_B = STG * STAGE_B * (SHARED ? 1 : NW);
     static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
