@@ -334,7 +334,7 @@ enum Held { kWords, kCodes8, kCodes4 };
 // their scales.  A word becomes eight 16-bit elements.
 //   UNITS: fp16 does not have the range of the scales.  There the elements are in units of the row's largest scale (of codes that are not
 //   zero), which the score is multiplied by; what is 2^-24 of it and less is lost.  bf16 has: the elements are the values.
-template <int D, int ROWS, bool UNITS>
+template <int D, int ROWS>
 struct Rows4 {
     static constexpr int ROWB = D / 2, PARTS = 64 / ROWS, WORDS = D == 64 && ROWS == 16 ? 2 : 4, CHUNKS = D / (8 * WORDS * PARTS);
     typedef __attribute__((ext_vector_type(WORDS))) int Chunk;
@@ -386,7 +386,7 @@ struct Rows4 {
         return __builtin_bit_cast(float, top == 255 ? 0x7FC00000 : top << 23);
     }
     // the eight elements of word U
-    template <int U>
+    template <int U, bool UNITS>
     __device__ __forceinline__ i32x4 operand() const {
         const float s = __builtin_bit_cast(float, scale[U / WORDS] << 23);
         const uint32_t w = (uint32_t)code[U / WORDS][U % WORDS];
@@ -398,15 +398,15 @@ struct Rows4 {
         });
         return y;
     }
-    // All 16 rows as 16-bit elements into a tile of type Tile, from its row 16 HALF on.  `to`: the lane's place for the word 0 of row lane % 16; the others are
-    // an exclusive or away, so 16 lanes of a write hit every bank once.
-    template <typename Tile, int HALF>
+    // All 16 rows as 16-bit elements into a tile.  `to`: the lane's place there for word 0 of row lane % 16; the others are an exclusive or
+    // away, so 16 lanes of a write hit every bank once.
+    template <bool UNITS, int FLIP = 0, int OFFSET = 0>
     __device__ __forceinline__ void put(uint32_t to) const {
         static_assert(ROWS == 16);
         typedef i32x4 __attribute__((address_space(3))) * lds_vec_ptr;
         static_for<CHUNKS * WORDS>([&](auto n) __attribute__((always_inline)) {
             constexpr int u = decltype(n)::value;
-            *(lds_vec_ptr)(uintptr_t)((to ^ (uint32_t)((u % WORDS ^ Tile::swizzle(16 * HALF)) << 4)) + (HALF * 32 * D + u / WORDS * 256)) = operand<u>();
+            *(lds_vec_ptr)(uintptr_t)((to ^ (uint32_t)((u % WORDS ^ FLIP) << 4)) + (OFFSET + u / WORDS * 256)) = operand<u, UNITS>();
         });
     }
 };
@@ -636,14 +636,15 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // e2m1: tiles on their way in registers, SETS of them.  kDivideKeys: K and V of the wave's own; kShareKeys: 16 rows of the tile that all
     // share, of K in waves 0 and 1 and of V in waves 2 and 3
     constexpr bool UNITS = FOUR && std::is_same_v<Tag, f16_tag>;
-    using Half = Rows4<D, 16, UNITS>;
-    using Keys = std::conditional_t<COLS == 16 || SHARED, Half, Rows4<D, 32, UNITS>>;
-    using Values = Rows4<D, 16, false>;
+    using Half = Rows4<D, 16>;
+    using Keys = std::conditional_t<COLS == 16 || SHARED, Half, Rows4<D, 32>>;
     constexpr int SETS = FOUR && COLS == 16 && D < 256 ? 2 : 1;  // (where two fit the registers)
     constexpr int KEY_TILES = COLS == 16 && !SHARED ? 2 : 1;
     Keys keys[SETS][KEY_TILES];
-    Values values[SETS][2];
-    const uint32_t put_at = tile.base + (lane & 15) * Tile::ROWB + (((Half::element(0, lane >> 4) / 8) ^ Tile::swizzle(lane & 15)) << 4);
+    Half values[SETS][SHARED ? 1 : 2];
+    const uint32_t put_at = tile.base + (lane & 15) * Tile::ROWB + (((Half::element(0, lane >> 4) / 8) ^ Tile::swizzle(lane & 15)) << 4) +
+                            (SHARED ? (wave & 1) * 16 * Tile::ROWB + (wave >> 1) * Tile::TILE_B : 0);
+    static_assert(!(FOUR && SHARED) || Tile::swizzle(16) == 0);
     struct TileRows {
         UniformRow lo, hi;
         __device__ __forceinline__ int bad() const { return (lo.none() & 1) | (hi.none() & 2); }
@@ -670,11 +671,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
             const long lo[1] = {at.lo.index()}, hi[1] = {at.hi.index()};
             if constexpr (SHARED) {
                 const long row[1] = {wave & 1 ? hi[0] : lo[0]};
-                if (wave & 2) to[0].request(a.c.v, a.c.v_scales, row, lane);
-                else keys[0][0].request(a.c.k, a.c.k_scales, row, lane);
+                to[0].request(wave & 2 ? a.c.v : a.c.k, wave & 2 ? a.c.v_scales : a.c.k_scales, row, lane);
             } else {
                 to[0].request(a.c.v, a.c.v_scales, lo, lane);
-                to[1].request(a.c.v, a.c.v_scales, hi, lane);
+                to[SHARED ? 0 : 1].request(a.c.v, a.c.v_scales, hi, lane);
             }
         }
     };
@@ -683,29 +683,24 @@ fa_fwd_cache_kernel(CachedArgs a) {
         if constexpr (FOUR) {
             const int there = key1 - (key0 + 32 * (kw + KW * i)), bad = at.bad();
             auto& v = values[decltype(set)::value];
+            const bool part_of_it = there < 32 || bad != 0;
             if constexpr (SHARED) {
-                const bool mine_is_there = (lane & 15) + 16 * (wave & 1) < there && !(bad >> (wave & 1) & 1);
-                const uint32_t to = put_at + offset;
-                if (wave & 2) {
-                    if (!mine_is_there) v[0].clear();
-                    if (wave & 1) v[0].template put<Tile, 1>(to + Tile::TILE_B);
-                    else v[0].template put<Tile, 0>(to + Tile::TILE_B);
+                if (part_of_it && !((lane & 15) + 16 * (wave & 1) < there && !(bad >> (wave & 1) & 1))) v[0].clear();
+                if (UNITS && wave < 2) {
+                    typedef float __attribute__((address_space(3))) * lds_float_ptr;
+                    const float unit = v[0].take_unit();
+                    if (lane < 16) *(lds_float_ptr)(uintptr_t)(tile.base + offset + 2 * Tile::TILE_B + 4 * (16 * (wave & 1) + lane)) = unit;
+                    v[0].template put<UNITS>(put_at + offset);
                 } else {
-                    if constexpr (UNITS) {
-                        typedef float __attribute__((address_space(3))) * lds_float_ptr;
-                        const float unit = keys[0][0].take_unit();
-                        if (lane < 16) *(lds_float_ptr)(uintptr_t)(tile.base + offset + 2 * Tile::TILE_B + 4 * (16 * (wave & 1) + lane)) = unit;
-                    }
-                    if (wave & 1) keys[0][0].template put<Tile, 1>(to);
-                    else keys[0][0].template put<Tile, 0>(to);
+                    v[0].template put<false>(put_at + offset);
                 }
             } else {
-                if (there < 32 || bad != 0) {
+                if (part_of_it) {
                     if (!((lane & 15) < there && !(bad & 1))) v[0].clear();
-                    if (!((lane & 15) + 16 < there && !(bad & 2))) v[1].clear();
+                    if (!((lane & 15) + 16 < there && !(bad & 2))) v[SHARED ? 0 : 1].clear();
                 }
-                v[0].template put<Tile, 0>(put_at + offset);
-                v[1].template put<Tile, 1>(put_at + offset);
+                v[0].template put<false>(put_at + offset);
+                v[SHARED ? 0 : 1].template put<false, Tile::swizzle(16), 16 * Tile::ROWB>(put_at + offset);
             }
         }
     };
@@ -808,7 +803,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
                         constexpr int u = decltype(n)::value;
                         static_for<M::TILES>([&](auto tile_no) __attribute__((always_inline)) {
                             constexpr int kt = decltype(tile_no)::value;
-                            const i32x4 w = codes[kt].template operand<u>();
+                            const i32x4 w = codes[kt].template operand<u, UNITS>();
 #pragma unroll
                             for (int x = 0; x < RT; ++x) y[x][kt] = MQ::mma(w, qreg[x][u], y[x][kt]);
                         });
