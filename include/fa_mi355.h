@@ -337,8 +337,9 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const void* k_scales
  * have to move they say which, and fa_cache_copy moves them, once for each layer whose pages go by the table.
  *   missing   : int32 [1] (device, written): how many pages were asked for and not there.  Their entries are -1: no page.
  *   src, dst  : int32 (device, written): the contents of page src[i] belong into page dst[i] now; -1 and -1: nothing to do
- *   workspace : device scratch of at least fa_cache_pages_workspace_bytes(B, n_pages) bytes (fa_cache_fork: B_new in place of B),
- *               16-byte aligned, owned by the caller; calls that may run at the same time need one each
+ *   workspace : device scratch of at least fa_cache_pages_workspace_bytes(B, n_pages) bytes (fa_cache_fork: B_new in place of B; it is 0
+ *               for small batches and pools: then workspace may be NULL), 16-byte aligned, owned by the caller; calls that may run at
+ *               the same time need one each
  * B * max_pages < 2^31.  Outputs overlap nothing else, but for new_table of fa_cache_compact, which may be block_table.  Free pages are
  * given in ascending order, to rows and their entries in order: the results are the same in every run.
  *

@@ -529,15 +529,24 @@ def _new(t, shape):
     return torch.empty(shape, device=t.device, dtype=torch.int32)
 
 
+def _together(like, *sized):
+    """The given tensors, and new ones of these sizes for those that are not, in one allocation"""
+    new = iter(_new(like, (sum(n for n, t in sized if t is None),)).split([n for n, t in sized if t is None]))
+    return [next(new) if t is None else t for _, t in sized]
+
+
 def fa_cache_pages_workspace_bytes(B, n_pages):
     return int(lib().fa_cache_pages_workspace_bytes(B, n_pages))
 
 
 def _pages_workspace(workspace, B, n_pages, like):
+    """(pointer, bytes, what keeps them) of the given workspace, or a new one where there has to be one"""
     if workspace is None:
-        return torch.empty((fa_cache_pages_workspace_bytes(B, n_pages),), device=like.device, dtype=torch.uint8)
-    _check("workspace", workspace, (workspace.numel(),), (torch.uint8,))
-    return workspace
+        need = fa_cache_pages_workspace_bytes(B, n_pages)
+        workspace = torch.empty((need,), device=like.device, dtype=torch.uint8) if need else None
+    else:
+        _check("workspace", workspace, (workspace.numel(),), (torch.uint8,))
+    return _ptr(workspace), 0 if workspace is None else workspace.numel(), workspace
 
 
 def _check_ints(*named):
@@ -566,13 +575,12 @@ def fa_cache_fork(block_table, lens, parents, page_size, n_pages, held=None, new
     (B, max_pages), B_new, n_pages = block_table.shape, parents.shape[0], int(n_pages)
     _check_ints(("lens", lens, (B,)), ("parents", parents, (B_new,)), ("held", held, (n_pages,)))
     new_table = _new(block_table, (B_new, max_pages)) if new_table is None else new_table
-    new_lens, src, dst = (_new(block_table, (B_new,)) if t is None else t for t in (new_lens, src, dst))
-    missing = _new(block_table, (1,)) if missing is None else missing
+    new_lens, src, dst, missing = _together(block_table, (B_new, new_lens), (B_new, src), (B_new, dst), (1, missing))
     _check_ints(("new_table", new_table, (B_new, max_pages)), ("new_lens", new_lens, (B_new,)), ("src", src, (B_new,)), ("dst", dst, (B_new,)),
                 ("missing", missing, (1,)))
-    workspace = _pages_workspace(workspace, B_new, n_pages, block_table)
+    space, bytes, workspace = _pages_workspace(workspace, B_new, n_pages, block_table)
     st = lib().fa_cache_fork(block_table.data_ptr(), lens.data_ptr(), parents.data_ptr(), _ptr(held), new_table.data_ptr(), new_lens.data_ptr(),
-                             src.data_ptr(), dst.data_ptr(), missing.data_ptr(), workspace.data_ptr(), workspace.numel(), B, B_new, int(page_size),
+                             src.data_ptr(), dst.data_ptr(), missing.data_ptr(), space, bytes, B, B_new, int(page_size),
                              n_pages, max_pages, _stream())
     if st != FA_OK:
         raise FaError(st, "fa_cache_fork")
@@ -590,9 +598,8 @@ def fa_cache_extend(block_table, lens, T, page_size, n_pages, counts=None, held=
     (B, max_pages), n_pages = block_table.shape, int(n_pages)
     missing = _new(block_table, (1,)) if missing is None else missing
     _check_ints(("lens", lens, (B,)), ("counts", counts, (B,)), ("held", held, (n_pages,)), ("missing", missing, (1,)))
-    workspace = _pages_workspace(workspace, B, n_pages, block_table)
-    st = lib().fa_cache_extend(block_table.data_ptr(), lens.data_ptr(), _ptr(counts), _ptr(held), missing.data_ptr(), workspace.data_ptr(),
-                               workspace.numel(), B, int(T), int(page_size), n_pages, max_pages, _stream())
+    space, bytes, workspace = _pages_workspace(workspace, B, n_pages, block_table)
+    st = lib().fa_cache_extend(block_table.data_ptr(), lens.data_ptr(), _ptr(counts), _ptr(held), missing.data_ptr(), space, bytes, B, int(T), int(page_size), n_pages, max_pages, _stream())
     if st != FA_OK:
         raise FaError(st, "fa_cache_extend")
     return block_table, missing
@@ -610,12 +617,11 @@ def fa_cache_compact(block_table, n_pages, moves=None, held=None, new_table=None
     moves = max(n_pages // 2, 1) if moves is None else int(moves)
     _check_ints(("held", held, (n_pages,)))
     new_table = _new(block_table, (B, max_pages)) if new_table is None else new_table
-    src, dst = (_new(block_table, (moves,)) if t is None else t for t in (src, dst))
-    top = _new(block_table, (1,)) if top is None else top
+    src, dst, top = _together(block_table, (moves, src), (moves, dst), (1, top))
     _check_ints(("new_table", new_table, (B, max_pages)), ("src", src, (moves,)), ("dst", dst, (moves,)), ("top", top, (1,)))
-    workspace = _pages_workspace(workspace, B, n_pages, block_table)
+    space, bytes, workspace = _pages_workspace(workspace, B, n_pages, block_table)
     st = lib().fa_cache_compact(block_table.data_ptr(), _ptr(held), new_table.data_ptr(), src.data_ptr(), dst.data_ptr(), top.data_ptr(),
-                                workspace.data_ptr(), workspace.numel(), B, moves, n_pages, max_pages, _stream())
+                                space, bytes, B, moves, n_pages, max_pages, _stream())
     if st != FA_OK:
         raise FaError(st, "fa_cache_compact")
     return new_table, src, dst, top

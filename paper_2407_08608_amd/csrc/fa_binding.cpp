@@ -615,8 +615,36 @@ const at::Tensor* table_of(Arguments& a, Py_ssize_t i, int device, int& B, int& 
     return fitting(a, i, device, {B, max_pages}, at::kInt);
 }
 const at::Tensor* ints_or_none(Arguments& a, Py_ssize_t i, int device, int64_t size) { return a.given(i) ? fitting(a, i, device, {size}, at::kInt) : nullptr; }
+// The given tensors of ints, and new ones of these sizes for those that are not, in one allocation
+template <size_t K>
+void together(Arguments& a, const Py_ssize_t (&index)[K], int device, const int64_t (&sizes)[K], const at::Tensor& like, at::Tensor (&out)[K]) {
+    int64_t total = 0, at = 0;
+    for (size_t i = 0; i < K; ++i) {
+        if (a.given(index[i])) {
+            const at::Tensor* t = fitting(a, index[i], device, {sizes[i]}, at::kInt);
+            if (t) out[i] = *t;
+        } else {
+            total += sizes[i];
+        }
+    }
+    if (!a.ok || total == 0) return;
+    const at::Tensor all = at::empty({total}, like.options());
+    for (size_t i = 0; i < K; ++i)
+        if (!a.given(index[i])) {
+            // (what a view does, without the dispatcher's microsecond)
+            auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+            impl->set_storage_offset(at);
+            impl->set_sizes_contiguous({sizes[i]});
+            out[i] = at::Tensor(std::move(impl));
+            at += sizes[i];
+        }
+}
+// (undefined where none is given and none is needed)
 at::Tensor pages_workspace(Arguments& a, Py_ssize_t i, int device, int B, int n_pages, const at::Tensor& like) {
-    if (!a.given(i)) return a.ok ? at::empty({(int64_t)lib.pages_workspace_bytes(B, n_pages)}, like.options().dtype(at::kByte)) : at::Tensor();
+    if (!a.given(i)) {
+        const int64_t need = a.ok ? (int64_t)lib.pages_workspace_bytes(B, n_pages) : 0;
+        return need > 0 ? at::empty({need}, like.options().dtype(at::kByte)) : at::Tensor();
+    }
     const at::Tensor* t = a.tensor(i);
     if (!t || t->device().index() != device || t->scalar_type() != at::kByte || t->dim() != 1) {
         a.ok = false;
@@ -642,15 +670,17 @@ PyObject* cache_fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor* held = ints_or_none(a, 5, device, n_pages);
         void* stream = a.stream(12);
         if (!a.ok) return nullptr;
-        const at::Tensor new_table = fitting_output(a, 6, device, {B_new, max_pages}, at::kInt, *table), new_lens = fitting_output(a, 7, device, {B_new}, at::kInt, *table),
-                         src = fitting_output(a, 8, device, {B_new}, at::kInt, *table), dst = fitting_output(a, 9, device, {B_new}, at::kInt, *table),
-                         missing = fitting_output(a, 10, device, {1}, at::kInt, *table);
+        const at::Tensor new_table = fitting_output(a, 6, device, {B_new, max_pages}, at::kInt, *table);
+        at::Tensor rest[4];
+        together(a, {7, 8, 9, 10}, device, {B_new, B_new, B_new, 1}, *table, rest);
+        if (!a.ok) return nullptr;
+        const at::Tensor &new_lens = rest[0], &src = rest[1], &dst = rest[2], &missing = rest[3];
         const at::Tensor workspace = pages_workspace(a, 11, device, B_new, n_pages, *table);
         if (!a.ok) return nullptr;
         const int *tp = pointer<int>(table), *lp = pointer<int>(lens), *pp = pointer<int>(parents), *hp = pointer<int>(held);
         int *ntp = pointer<int>(&new_table), *nlp = pointer<int>(&new_lens), *sp = pointer<int>(&src), *dp = pointer<int>(&dst), *mp = pointer<int>(&missing);
-        void* wp = workspace.data_ptr();
-        const size_t bytes = (size_t)workspace.numel();
+        void* wp = workspace.defined() ? workspace.data_ptr() : nullptr;
+        const size_t bytes = workspace.defined() ? (size_t)workspace.numel() : 0;
         const int st = without_gil([&] {
             return lib.cache_fork(tp, lp, pp, hp, ntp, nlp, sp, dp, mp, wp, bytes, B, B_new, page_size, n_pages, max_pages, stream);
         });
@@ -676,8 +706,8 @@ PyObject* cache_extend(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!a.ok) return nullptr;
         int *tp = pointer<int>(table), *mp = pointer<int>(&missing);
         const int *lp = pointer<int>(lens), *cp = pointer<int>(counts), *hp = pointer<int>(held);
-        void* wp = workspace.data_ptr();
-        const size_t bytes = (size_t)workspace.numel();
+        void* wp = workspace.defined() ? workspace.data_ptr() : nullptr;
+        const size_t bytes = workspace.defined() ? (size_t)workspace.numel() : 0;
         const int st = without_gil([&] { return lib.cache_extend(tp, lp, cp, hp, mp, wp, bytes, B, T, page_size, n_pages, max_pages, stream); });
         return result(st, a, {0, 7}, {*table, missing});
     });
@@ -695,14 +725,17 @@ PyObject* cache_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor* held = ints_or_none(a, 3, device, n_pages);
         void* stream = a.stream(9);
         if (!a.ok) return nullptr;
-        const at::Tensor new_table = fitting_output(a, 4, device, {B, max_pages}, at::kInt, *table), src = fitting_output(a, 5, device, {moves}, at::kInt, *table),
-                         dst = fitting_output(a, 6, device, {moves}, at::kInt, *table), top = fitting_output(a, 7, device, {1}, at::kInt, *table);
+        const at::Tensor new_table = fitting_output(a, 4, device, {B, max_pages}, at::kInt, *table);
+        at::Tensor rest[3];
+        together(a, {5, 6, 7}, device, {moves, moves, 1}, *table, rest);
+        if (!a.ok) return nullptr;
+        const at::Tensor &src = rest[0], &dst = rest[1], &top = rest[2];
         const at::Tensor workspace = pages_workspace(a, 8, device, B, n_pages, *table);
         if (!a.ok) return nullptr;
         const int *tp = pointer<int>(table), *hp = pointer<int>(held);
         int *ntp = pointer<int>(&new_table), *sp = pointer<int>(&src), *dp = pointer<int>(&dst), *top_p = pointer<int>(&top);
-        void* wp = workspace.data_ptr();
-        const size_t bytes = (size_t)workspace.numel();
+        void* wp = workspace.defined() ? workspace.data_ptr() : nullptr;
+        const size_t bytes = workspace.defined() ? (size_t)workspace.numel() : 0;
         const int st = without_gil([&] { return lib.cache_compact(tp, hp, ntp, sp, dp, top_p, wp, bytes, B, moves, n_pages, max_pages, stream); });
         return result(st, a, {4, 5, 6, 7}, {new_table, src, dst, top});
     });

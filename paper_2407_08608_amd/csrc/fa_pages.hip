@@ -14,14 +14,17 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kWindow = 1 << 18;  // pages whose bits are in the LDS at a time
-constexpr int kListed = 1024;     // rows, and free pages, that are kept in the LDS and not in the workspace
+constexpr int kListed = 1024;     // rows whose numbers are kept in the LDS and not in the workspace
+constexpr int kSmallPool = 4096;  // pages whose lists are
 constexpr int kHead = 16;
 
-// The workspace, in ints: a head, three lists of pages, two of rows
+constexpr bool small(int B, int n_pages) { return B <= kListed && n_pages <= kSmallPool; }
+
+// In the workspace, or where that is none in the LDS, in ints: a head, three lists of pages, two of rows
 struct Lists {
     int *head, *free, *high, *to, *part, *need;
-    __host__ __device__ Lists(void* workspace, int B, int n_pages) {
-        head = static_cast<int*>(workspace);
+    __device__ Lists(void* at, int B, int n_pages) {
+        head = static_cast<int*>(at);
         free = head + kHead;
         high = free + n_pages;
         to = high + n_pages;
@@ -29,6 +32,7 @@ struct Lists {
         need = part + B;
     }
 };
+constexpr size_t list_ints(int B, int n_pages) { return kHead + 3 * (size_t)n_pages + 2 * (size_t)B; }
 
 struct Pool {
     const int* held;  // [n_pages] or NULL
@@ -39,12 +43,15 @@ struct Pool {
 
 struct Shared {
     int sums[kWaves + 1];
-    int part[kListed], need[kListed], list[kListed], parent[kListed], whole[kListed];
-    uint32_t bits[1];  // kWindow / 32, or as many as the pool has; a compaction: twice
+    int whole[kListed], seen[kListed];
+    uint32_t bits[1];  // kWindow / 32, or as many as the pool has; a compaction: twice.  Behind them the lists, where there is no workspace.
 };
-constexpr size_t shared_bytes(int n_pages, int bitmaps) {
-    const int n = n_pages < kWindow ? n_pages : kWindow;
-    return sizeof(Shared) + (size_t)((n + 31) / 32) * 4 * bitmaps;
+constexpr int bitmap_words(int n_pages) { return ((n_pages < kWindow ? n_pages : kWindow) + 31) / 32; }
+constexpr size_t shared_bytes(int B, int n_pages, int bitmaps) {
+    return sizeof(Shared) + 4 * ((size_t)bitmap_words(n_pages) * bitmaps + (small(B, n_pages) ? list_ints(B, n_pages) : 0));
+}
+static __device__ __forceinline__ Lists lists_of(Shared& s, void* workspace, int B, int n_pages, int bitmaps) {
+    return Lists(small(B, n_pages) ? static_cast<void*>(s.bits + bitmap_words(n_pages) * bitmaps) : workspace, B, n_pages);
 }
 
 // The sum of x over the threads before this one, and over all
@@ -81,16 +88,36 @@ static __device__ __forceinline__ void clear(uint32_t* bits, int words) {
     __syncthreads();
 }
 
+// f(number, value) of n ints, 16 of a thread on their way at a time: one workgroup has nothing else to hide a read of memory behind
+template <typename F>
+static __device__ __forceinline__ void for_each_int(const int* p, int n, F&& f) {
+    const int skip = min((int)(-(reinterpret_cast<uintptr_t>(p) / 4) & 3), n), whole = (n - skip) / 4;  // to where four ints are aligned
+    const i32x4* const x = reinterpret_cast<const i32x4*>(p + skip);
+    const int rest = skip + 4 * whole;
+    if ((int)threadIdx.x < skip) f((int)threadIdx.x, p[threadIdx.x]);
+    if ((int)threadIdx.x < n - rest) f(rest + (int)threadIdx.x, p[rest + threadIdx.x]);
+    constexpr int AHEAD = 4;
+    for (int i0 = threadIdx.x; i0 < whole; i0 += AHEAD * kThreads) {
+        i32x4 v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) v[j] = x[min(i0 + j * kThreads, whole - 1)];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i0 + j * kThreads < whole)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(skip + 4 * (i0 + j * kThreads) + e, v[j][e]);
+    }
+}
+
 // What the caller holds, and all entries of a table
 static __device__ __forceinline__ void mark_held(uint32_t* bits, const Pool& pool, int base, int n) {
-    if (!pool.held) return;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (pool.held[base + i] != 0) mark(bits, i, 0, n);
+    if (pool.held)
+        for_each_int(pool.held + base, n, [&](int page, int held) {
+            if (held != 0) mark(bits, page, 0, n);
+        });
 }
 static __device__ __forceinline__ void mark_table(uint32_t* bits, const int* table, int entries, int base, int n) {
-#pragma unroll 8
-    for (int i = threadIdx.x; i < entries; i += kThreads) mark(bits, table[i], base, n);
+    for_each_int(table, entries, [&](int, int page) { mark(bits, page, base, n); });
 }
 
 // The pages base .. base + n - 1 whose bit is `value` (and whose bit in `others` is not set) go to list[found ..] in ascending order, up to `most`
@@ -151,24 +178,30 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
     }
     extern __shared__ char raw[];
     Shared& s = *reinterpret_cast<Shared*>(raw);
-    const Lists lists(a.workspace, a.B_new, pool.n_pages);
-    const bool few = a.B_new <= kListed;
-    int *const part = few ? s.part : lists.part, *const need = few ? s.need : lists.need, *const list = few ? s.list : lists.free;
+    const Lists lists = lists_of(s, a.workspace, a.B_new, pool.n_pages, 1);
+    int *const part = lists.part, *const need = lists.need, *const list = lists.free;
     const int tid = threadIdx.x;
 
     // The pages that new sequences would write to, and whether an earlier one does: that keeps it, the others need a copy
+    const bool once = a.B <= kListed;  // what is whole of each old sequence that is continued is written down here, and not for each window again
+    if (once) {
+        if (tid < a.B) s.whole[tid] = 0;
+        __syncthreads();
+    }
     for (int i = tid; i < a.B_new; i += kThreads) {
         const Continued c(a, i);
+        if (once && c.parent >= 0) s.whole[c.parent] = c.whole;  // (the same from all)
         const int page = c.last ? a.table[(long)c.parent * pool.max_pages + c.whole] : -1;
         part[i] = pool.has(page) ? page : -1;
+        if (i < kListed) s.seen[i] = part[i];
     }
     __syncthreads();
-    if (few) {
+    if (a.B_new <= kListed) {
         if (tid < a.B_new) {
-            const int page = s.part[tid];
+            const int page = part[tid];
             bool earlier = false;
-            for (int j = 0; j < tid; ++j) earlier |= s.part[j] == page;
-            s.need[tid] = page >= 0 && earlier;
+            for (int j = 0; j < tid; ++j) earlier |= s.seen[j] == page;
+            need[tid] = page >= 0 && earlier;
         }
     } else {
         int* const first = lists.high;
@@ -188,19 +221,35 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
     for (int base = 0; base < pool.n_pages; base += kWindow) {
         const int n = min(kWindow, pool.n_pages - base);
         clear(s.bits, (n + 31) / 32);
-        for (int r0 = 0; r0 < a.B_new; r0 += kListed) {
-            const int rows = min(kListed, a.B_new - r0);
-            for (int i = tid; i < rows; i += kThreads) {
-                const Continued c(a, r0 + i);
-                s.parent[i] = c.parent;
-                s.whole[i] = c.whole;
+        // The whole pages of old sequences that are continued, each looked at once however many continue it: a wave takes 512 entries of a
+        // row, two rows' at a time
+        for (int r0 = 0; r0 < a.B; r0 += kListed) {
+            const int rows = min(kListed, a.B - r0);
+            if (!once) {
+                for (int i = tid; i < rows; i += kThreads) s.whole[i] = 0;
+                __syncthreads();
+                for (int i = tid; i < a.B_new; i += kThreads) {
+                    const Continued c(a, i);
+                    if (c.parent >= r0 && c.parent - r0 < rows) s.whole[c.parent - r0] = c.whole;
+                }
+                __syncthreads();
             }
-            __syncthreads();
-            const unsigned entries = (unsigned)rows * pool.max_pages;
-#pragma unroll 4
-            for (unsigned i = tid; i < entries; i += kThreads) {
-                const int row = i / (unsigned)pool.max_pages, e = i - row * pool.max_pages;
-                if (e < s.whole[row]) mark(s.bits, a.table[(long)s.parent[row] * pool.max_pages + e], base, n);
+            const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), parts = (pool.max_pages + 511) / 512;
+            const unsigned units = (unsigned)rows * parts;
+            for (unsigned u0 = wave; u0 < units; u0 += 2 * kWaves) {
+                int page[2][8];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const unsigned u = min(u0 + x * kWaves, units - 1);
+                    const int row = u / (unsigned)parts, e0 = (u - row * parts) * 512 + lane, whole = s.whole[row];
+                    const int* const entries = a.table + (long)(r0 + row) * pool.max_pages;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) page[x][j] = e0 + 64 * j < whole ? entries[e0 + 64 * j] : -1;
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) mark(s.bits, page[x][j], base, n);
             }
             __syncthreads();
         }
@@ -276,7 +325,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
         return;
     }
     const int most = min(wanted, pool.n_pages);
-    int* const list = most <= kListed ? s.list : Lists(a.workspace, a.B, pool.n_pages).free;
+    int* const list = lists_of(s, a.workspace, a.B, pool.n_pages, 1).free;
     int found = 0;
     for (int base = 0; base < pool.n_pages; base += kWindow) {
         const int n = min(kWindow, pool.n_pages - base);
@@ -314,7 +363,7 @@ struct CompactArgs {
     const int* table;
     int *new_table, *src, *dst, *top;
     void* workspace;
-    int B, moves;
+    int B, moves, renumbers;  // whether the one workgroup sees to the table too
     Pool pool;
 };
 
@@ -323,8 +372,8 @@ __global__ void __launch_bounds__(kThreads) fa_cache_compact_kernel(CompactArgs 
     const Pool& pool = a.pool;
     extern __shared__ char raw[];
     Shared& s = *reinterpret_cast<Shared*>(raw);
-    const Lists lists(a.workspace, a.B, pool.n_pages);
-    const int tid = threadIdx.x, half = (min(kWindow, pool.n_pages) + 31) / 32;
+    const Lists lists = lists_of(s, a.workspace, a.B, pool.n_pages, 2);
+    const int tid = threadIdx.x, half = bitmap_words(pool.n_pages);
     uint32_t *const used = s.bits, *const held = s.bits + half;
     int n_free = 0, n_high = 0, top_held = -1;
     for (int base = 0; base < pool.n_pages; base += kWindow) {
@@ -344,37 +393,49 @@ __global__ void __launch_bounds__(kThreads) fa_cache_compact_kernel(CompactArgs 
         __syncthreads();
     }
     const int most = min(min(n_free, n_high), a.moves);
-    int moved = 0;
-    for (int k0 = 0; k0 < a.moves; k0 += kThreads) {
-        const int k = k0 + tid;
-        int from = -1, to = -1;
-        if (k < most) {
-            from = lists.high[n_high - 1 - k];
-            to = lists.free[k];
-            if (to > from) from = to = -1;
+    int mine = 0, moved;
+    constexpr int AHEAD = 4;
+    for (int k0 = tid; k0 < a.moves; k0 += AHEAD * kThreads) {
+        int from[AHEAD], to[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int k = k0 + j * kThreads;
+            from[j] = k < most ? lists.high[n_high - 1 - k] : -1;
+            to[j] = k < most ? lists.free[k] : 0;
         }
-        if (k < a.moves) {
-            a.src[k] = from;
-            a.dst[k] = to;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int k = k0 + j * kThreads;
+            const bool moves = to[j] < from[j];  // (once one does not, none after it does)
+            if (k < a.moves) {
+                a.src[k] = moves ? from[j] : -1;
+                a.dst[k] = moves ? to[j] : -1;
+            }
+            if (moves) lists.to[from[j]] = to[j];
+            mine += moves;
         }
-        if (from >= 0) lists.to[from] = to;
-        int all;
-        sum_before(from >= 0, all, s.sums);
-        moved += all;
     }
-    s.list[tid] = top_held;
+    sum_before(mine, moved, s.sums);
+    int* const tops = s.whole;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) top_held = max(top_held, __shfl_xor(top_held, d));
+    if ((tid & 63) == 0) tops[tid >> 6] = top_held;
     __syncthreads();
-    for (int d = kThreads / 2; d > 0; d /= 2) {
-        if (tid < d) s.list[tid] = max(s.list[tid], s.list[tid + d]);
-        __syncthreads();
-    }
+    const int threshold = moved > 0 ? lists.high[n_high - moved] : 0x7fffffff;  // pages from here on have moved, but for held ones
     if (tid == 0) {
-        int top = s.list[0];
+        int top = tops[0];
+        for (int w = 1; w < kWaves; ++w) top = max(top, tops[w]);
         if (n_high > moved) top = max(top, lists.high[n_high - 1 - moved]);
         if (moved > 0) top = max(top, lists.free[moved - 1]);
         *a.top = top + 1;
-        lists.head[0] = moved > 0 ? lists.high[n_high - moved] : 0x7fffffff;  // pages from here on have moved, but for held ones
+        lists.head[0] = threshold;
     }
+    if (!a.renumbers) return;
+    const int entries = a.B * pool.max_pages;
+    for_each_int(a.table, entries, [&](int i, int page) {
+        if (pool.has(page) && page >= threshold && !(pool.held && pool.held[page] != 0)) page = lists.to[page];
+        a.new_table[i] = page;
+    });
 }
 
 __global__ void __launch_bounds__(256) fa_cache_renumber_kernel(CompactArgs a) {
@@ -388,23 +449,24 @@ __global__ void __launch_bounds__(256) fa_cache_renumber_kernel(CompactArgs a) {
 
 // ------------------------------------------------------------------------------------------
 
-// A workgroup brings 16 KiB of K or V of a pair's page, and the first one of each its scales
-constexpr int kChunk = 16384;
+// A workgroup brings 4 AT_ONCE KiB of K or V of a pair's page, and the first one of each its scales.  us, 4 / 2: 112 pairs of 64 KiB each 8.4 /
+// 6.8, where all workgroups there are start at once; 1700 of 3838 pairs of 32 KiB 41.9 / 45.3
+template <int AT_ONCE>
 __global__ void __launch_bounds__(256) fa_cache_copy_kernel(Cache c, const int* src, const int* dst, unsigned chunks, long bytes, long scale_bytes) {
     const unsigned part = blockIdx.x % (2 * chunks), pair = blockIdx.x / (2 * chunks);
     const int from = src[pair], to = dst[pair];
     if ((unsigned)from >= (unsigned)c.n_pages || (unsigned)to >= (unsigned)c.n_pages || from == to) return;
     const bool v = part >= chunks;
     char* const pages = static_cast<char*>(v ? c.v : c.k);
-    const long first = (long)(v ? part - chunks : part) * kChunk + threadIdx.x * 16;
+    const long first = (long)(v ? part - chunks : part) * (4096 * AT_ONCE) + threadIdx.x * 16;
     const char* x = pages + from * bytes;
     char* y = pages + to * bytes;
-    i32x4 w[4];
+    i32x4 w[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < AT_ONCE; ++i)
         if (first + i * 4096 < bytes) w[i] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(x + first + i * 4096));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < AT_ONCE; ++i)
         if (first + i * 4096 < bytes) __builtin_nontemporal_store(w[i], reinterpret_cast<i32x4*>(y + first + i * 4096));
     if (scale_bytes > 0 && part % chunks == 0) {
         char* const scales = static_cast<char*>(v ? c.v_scales : c.k_scales);
@@ -417,29 +479,31 @@ int launched() { return hipGetLastError() == hipSuccess ? FA_OK : FA_ERR_LAUNCH;
 
 }  // namespace
 
-size_t cache_pages_workspace_bytes(int B, int n_pages) { return sizeof(int) * (kHead + 3 * (size_t)n_pages + 2 * (size_t)B); }
+size_t cache_pages_workspace_bytes(int B, int n_pages) { return small(B, n_pages) ? 0 : sizeof(int) * list_ints(B, n_pages); }
 
 int launch_cache_fork(const int* block_table, const int* lens, const int* parents, const int* held, int* new_table, int* new_lens, int* src,
                       int* dst, int* missing, void* workspace, int B, int B_new, int page_size, int n_pages, int max_pages, hipStream_t stream) {
     const ForkArgs a = {block_table, lens, parents, new_table, new_lens, src, dst, missing, workspace, B, B_new, {held, n_pages, max_pages, page_size}};
     const long total = (long)B_new * max_pages, each = kThreads * kPerThread;
-    hipLaunchKernelGGL(fa_cache_fork_kernel, dim3((unsigned)(1 + (total + each - 1) / each)), dim3(kThreads), shared_bytes(n_pages, 1), stream, a);
+    hipLaunchKernelGGL(fa_cache_fork_kernel, dim3((unsigned)(1 + (total + each - 1) / each)), dim3(kThreads), shared_bytes(B_new, n_pages, 1), stream, a);
     return launched();
 }
 
 int launch_cache_extend(int* block_table, const int* lens, const int* counts, const int* held, int* missing, void* workspace, int B, int T,
                         int page_size, int n_pages, int max_pages, hipStream_t stream) {
     const ExtendArgs a = {block_table, lens, counts, missing, workspace, B, T, {held, n_pages, max_pages, page_size}};
-    hipLaunchKernelGGL(fa_cache_extend_kernel, dim3(1), dim3(kThreads), shared_bytes(n_pages, 1), stream, a);
+    hipLaunchKernelGGL(fa_cache_extend_kernel, dim3(1), dim3(kThreads), shared_bytes(B, n_pages, 1), stream, a);
     return launched();
 }
 
 int launch_cache_compact(const int* block_table, const int* held, int* new_table, int* src, int* dst, int* top, void* workspace, int B,
                          int moves, int n_pages, int max_pages, hipStream_t stream) {
-    const CompactArgs a = {block_table, new_table, src, dst, top, workspace, B, moves, {held, n_pages, max_pages, 0}};
-    hipLaunchKernelGGL(fa_cache_compact_kernel, dim3(1), dim3(kThreads), shared_bytes(n_pages, 2), stream, a);
+    // (a second launch costs 2 to 3 us; one workgroup takes that long for some 16 thousand entries.  It needs the lists in a workspace.)
+    const int renumbers = small(B, n_pages) || (long)B * max_pages <= 16384;
+    const CompactArgs a = {block_table, new_table, src, dst, top, workspace, B, moves, renumbers, {held, n_pages, max_pages, 0}};
+    hipLaunchKernelGGL(fa_cache_compact_kernel, dim3(1), dim3(kThreads), shared_bytes(B, n_pages, 2), stream, a);
     const int st = launched();
-    if (st != FA_OK) return st;
+    if (st != FA_OK || renumbers) return st;
     const long total = (long)B * max_pages;
     hipLaunchKernelGGL(fa_cache_renumber_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, stream, a);
     return launched();
@@ -449,10 +513,14 @@ int launch_cache_copy(const Cache& cache, const int* src, const int* dst, int n,
     const long rows = (long)cache.H_kv * cache.page_size;
     const long bytes = rows * (cache.dtype == FA_FP4_E2M1 ? d / 2 : cache.dtype == FA_FP8_E4M3 ? d : 2 * d);
     const long scale_bytes = rows * (cache.dtype == FA_FP4_E2M1 ? d / 32 : cache.dtype == FA_FP8_E4M3 ? 4 : 0);
-    const long chunks = (bytes + kChunk - 1) / kChunk;
-    if ((double)n * 2 * chunks * 256 >= 4294967296.0) return FA_ERR_LAUNCH;
-    hipLaunchKernelGGL(fa_cache_copy_kernel, dim3((unsigned)(n * 2 * chunks)), dim3(256), 0, stream, cache, src, dst, (unsigned)chunks, bytes, scale_bytes);
-    return launched();
+    auto go = [&](auto at_once, auto kernel) {
+        const long each = 4096 * decltype(at_once)::value, chunks = (bytes + each - 1) / each;
+        if ((double)n * 2 * chunks * 256 >= 4294967296.0) return (int)FA_ERR_LAUNCH;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(n * 2 * chunks)), dim3(256), 0, stream, cache, src, dst, (unsigned)chunks, bytes, scale_bytes);
+        return launched();
+    };
+    if ((double)n * 2 * bytes > 64.0 * 1024 * 1024) return go(std::integral_constant<int, 4>{}, fa_cache_copy_kernel<4>);
+    return go(std::integral_constant<int, 2>{}, fa_cache_copy_kernel<2>);
 }
 
 }  // namespace fa

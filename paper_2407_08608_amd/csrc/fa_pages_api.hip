@@ -26,7 +26,9 @@ int check_pool(int B, int n_pages, int max_pages) {
     return FA_OK;
 }
 int check_workspace(const void* workspace, size_t bytes, int B, int n_pages) {
-    if (!workspace || bytes < fa::cache_pages_workspace_bytes(B, n_pages)) return FA_ERR_WORKSPACE;
+    const size_t need = fa::cache_pages_workspace_bytes(B, n_pages);
+    if (need == 0) return FA_OK;
+    if (!workspace || bytes < need) return FA_ERR_WORKSPACE;
     return aligned16(workspace) ? FA_OK : FA_ERR_ALIGN;
 }
 

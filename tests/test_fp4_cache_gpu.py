@@ -318,7 +318,7 @@ def test_a_captured_step_with_pages_positions_and_attention():
     axis = (torch.arange(d // 2, device="cuda") % 3).int()
     outs = [torch.zeros_like(q), torch.zeros((B, H, T), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")]
     qr, kr = torch.zeros_like(q), torch.zeros_like(k)
-    pool_space = torch.empty(binding.fa_cache_pages_workspace_bytes(B, n_pages), dtype=torch.uint8, device="cuda")
+    pool_space = torch.empty(max(binding.fa_cache_pages_workspace_bytes(B, n_pages), 16), dtype=torch.uint8, device="cuda")
     space = torch.empty(max(binding.fa_fwd_cache_workspace_bytes(B, H, H_kv, T, d, wide * page, binding.FA_FP4_E2M1), 16), dtype=torch.uint8, device="cuda")
 
     def step():

@@ -36,7 +36,7 @@ def _same(got, want):
 
 
 # rows, new rows, width, page, pages of the pool
-_SIZES = [(1, 1, 1, 16, 1), (1, 1, 1, 16, 2), (2, 5, 3, 16, 40), (4, 16, 7, 1, 100), (16, 16, 20, 16, 700), (7, 3, 33, 48, 300), (64, 64, 9, 16, 601),
+_SIZES = [(1025, 3, 2, 16, 4000), (5, 1025, 4, 16, 4096), (30, 40, 150, 16, 4097), (1, 1, 1, 16, 1), (1, 1, 1, 16, 2), (2, 5, 3, 16, 40), (4, 16, 7, 1, 100), (16, 16, 20, 16, 700), (7, 3, 33, 48, 300), (64, 64, 9, 16, 601),
           (3, 1500, 2, 16, 4000), (1030, 1025, 3, 5, 5000), (5, 9, 300, 64, 1100)]
 
 
@@ -207,7 +207,7 @@ def test_replayed_steps_and_another_stream():
     own = g.permutation(n_pages)[:B * wide].reshape(B, wide)
     table, lens, parents = _ints(own), _ints([0] * B), _ints([0] * B)
     out = [_ints(np.zeros(s)) for s in ((B, wide), B, B, B, 1, 1)]
-    space = torch.empty(binding.fa_cache_pages_workspace_bytes(B, n_pages), dtype=torch.uint8, device="cuda")
+    space = torch.empty(max(binding.fa_cache_pages_workspace_bytes(B, n_pages), 16), dtype=torch.uint8, device="cuda")
 
     def step():
         binding.fa_cache_fork(table, lens, parents, page, n_pages, new_table=out[0], new_lens=out[1], src=out[2], dst=out[3], missing=out[4], workspace=space)
@@ -250,7 +250,7 @@ def test_the_binding_refuses_what_does_not_fit():
     for call, kind in ((lambda: fork(t.long(), lens, p, 16, 9), ValueError), (lambda: fork(t, lens[:2], p, 16, 9), ValueError),
                        (lambda: fork(t, lens, p[None], 16, 9), ValueError), (lambda: fork(t, lens, p.cpu(), 16, 9), ValueError),
                        (lambda: fork(t, lens, p, 0, 9), binding.FaError), (lambda: fork(t, lens, p, 16, 0), binding.FaError),
-                       (lambda: fork(t, lens, p, 16, 9, held=lens), ValueError), (lambda: fork(t, lens, p, 16, 9, workspace=small), binding.FaError),
+                       (lambda: fork(t, lens, p, 16, 9, held=lens), ValueError), (lambda: fork(t, lens, p, 16, 5000, workspace=small), binding.FaError),
                        (lambda: fork(t, lens, _ints([0, 1, 2]), 16, 9, new_table=t), binding.FaError),
                        (lambda: fork(t, lens, p[:0], 16, 9), binding.FaError), (lambda: fork(t, lens, p, 16, 9, src=lens), ValueError),
                        (lambda: binding.fa_cache_extend(t, lens, 0, 16, 9), binding.FaError), (lambda: binding.fa_cache_extend(t, lens, 1, 16, 9, counts=p), ValueError),

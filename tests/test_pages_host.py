@@ -86,7 +86,7 @@ def _compact(**kw):
     (c, kw, s) for c, ptrs in ((_fork, ("table", "lens", "parents", "new", "new_lens", "src", "dst", "missing")), (_extend, ("table", "lens", "missing")),
                                (_compact, ("table", "new", "src", "dst", "top"))) for kw, s in
     [({p: None}, 1) for p in ptrs] + [({p: P + 2}, 5) for p in ptrs + ("held",)] +
-    [(dict(B=0), 2), (dict(n_pages=0), 2), (dict(max_pages=0), 2), (dict(B=1 << 16, max_pages=1 << 15), 2), (dict(ws=None), 6), (dict(bytes=3), 6), (dict(ws=P + 8), 5)]
+    [(dict(B=0), 2), (dict(n_pages=0), 2), (dict(max_pages=0), 2), (dict(B=1 << 16, max_pages=1 << 15), 2), (dict(ws=None, n_pages=5000), 6), (dict(bytes=3, n_pages=5000), 6), (dict(ws=P + 8, n_pages=5000), 5)]
 ] + [(_fork, dict(B_new=0), 2), (_fork, dict(B_new=-1), 2), (_fork, dict(page=0), 2), (_fork, dict(page=1 << 16, max_pages=1 << 15), 2), (_fork, dict(new=P), 2),
      (_fork, dict(B_new=1 << 16, max_pages=1 << 15), 2), (_extend, dict(T=0), 2), (_extend, dict(page=-1), 2), (_extend, dict(B=3, T=1 << 30), 2),
      (_extend, dict(counts=P + 1), 5), (_compact, dict(moves=0), 2), (_compact, dict(moves=-5), 2)])
@@ -96,9 +96,11 @@ def test_pages_refuse_before_any_launch(call, kw, status):
 
 def test_workspace_of_pages():
     W = binding.fa_cache_pages_workspace_bytes
-    assert W(0, 9) == 0 and W(3, 0) == 0 and W(3, 9) >= 4 * 27
-    need = W(4, 9)
-    assert _fork(bytes=need - 1) == 6 and _extend(B=4, bytes=need - 1) == 6 and _compact(B=4, bytes=need - 1) == 6
+    assert W(0, 9) == 0 and W(3, 0) == 0 and W(3, 9) == 0 and W(1024, 4096) == 0 and W(1025, 9) >= 4 * 27 and W(3, 4097) >= 4 * 3 * 4097
+    for B, n_pages in ((2000, 9), (4, 100000)):
+        need = W(B, n_pages)
+        assert _fork(B_new=B, n_pages=n_pages, bytes=need - 1) == 6 and _extend(B=B, n_pages=n_pages, bytes=need - 1) == 6
+        assert _compact(B=B, n_pages=n_pages, bytes=need - 1) == 6
 
 
 def test_the_binding_refuses_tensors_that_are_not_on_a_device():
