@@ -88,7 +88,7 @@ template <int DTYPE> struct Elements {
     }
 };
 
-// 16 elements as e2m1 codes, which the instructions convert from and to values over a scale (to nearest even; to +-6 above 5)
+// 16 elements as e2m1 codes, which the instructions convert from and to values over a scale
 template <> struct Elements<FA_FP4_E2M1> {
     static constexpr int BYTES = 8;
     i32x2 w;
@@ -112,11 +112,18 @@ template <> struct Elements<FA_FP4_E2M1> {
     __device__ __forceinline__ void get(float (&f)[16], float scale) const {
         static_for<8>([&](auto t) __attribute__((always_inline)) { get2<decltype(t)::value>(f, scale); });
     }
-    __device__ __forceinline__ void set(const float (&f)[16]) {
+    // from the elements as they are, over `scale`
+    template <int DTYPE>
+    __device__ __forceinline__ void set(const Elements<DTYPE>& x, float scale) {
         uint32_t u[2] = {0, 0};
         static_for<8>([&](auto t) __attribute__((always_inline)) {
             constexpr int T = decltype(t)::value;
-            u[T / 4] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u[T / 4], f[2 * T], f[2 * T + 1], 1.0f, T % 4);
+            if constexpr (DTYPE == FA_F32)
+                u[T / 4] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u[T / 4], __builtin_bit_cast(float, (int)x.w[T / 2][2 * T % 4]),
+                                                                    __builtin_bit_cast(float, (int)x.w[T / 2][2 * T % 4 + 1]), scale, T % 4);
+            else if constexpr (DTYPE == FA_BF16)
+                u[T / 4] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(u[T / 4], __builtin_bit_cast(bf16x2, (int)x.w[T / 4][T % 4]), scale, T % 4);
+            else u[T / 4] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(u[T / 4], __builtin_bit_cast(f16x2, (int)x.w[T / 4][T % 4]), scale, T % 4);
         });
         w = i32x2{(int)u[0], (int)u[1]};
     }
@@ -151,23 +158,45 @@ static __device__ __forceinline__ float quantise(float (&f)[16]) {
     return a > 0.f ? a / kE4m3Max : 1.f;
 }
 
-// Values of a half of 32 elements (the other is the neighbouring lane's), in units of their scale, and the scale's biased exponent: of
-// the least power of two s with a <= 7 s, where 7 is what still rounds to the largest code, 6, by no more than half a step
-static __device__ __forceinline__ uint32_t quantise_32(float (&f)[16]) {
-    float a = 0.f;
-    bool nan = false;
+// The bits of the largest magnitude of 16 elements and the neighbouring lane's 16, in their own type; without FINITE infinities and NaN
+// count as what their bits say, which is more than any number
+template <bool FINITE, int DTYPE>
+static __device__ __forceinline__ uint32_t largest_of_32(const Elements<DTYPE>& x) {
+    uint32_t top = 0;
+    if constexpr (DTYPE == FA_F32) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-        a = fmaxf(a, fabsf(f[t]) < INFINITY ? fabsf(f[t]) : 0.f);
-        nan |= f[t] != f[t];
+        for (int t = 0; t < 16; ++t) {
+            const uint32_t u = (uint32_t)x.w[t / 4][t % 4] & 0x7FFFFFFFu;
+            top = max(top, FINITE && u >= 0x7F800000u ? 0u : u);
+        }
+    } else {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+        constexpr uint16_t inf = DTYPE == FA_BF16 ? 0x7F80 : 0x7C00;
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            u16x2 u = __builtin_bit_cast(u16x2, (uint32_t)x.w[t / 4][t % 4] & 0x7FFF7FFFu);
+            if (FINITE) u = u16x2{(uint16_t)(u[0] >= inf ? 0 : u[0]), (uint16_t)(u[1] >= inf ? 0 : u[1])};
+            m = __builtin_elementwise_max(m, u);
+        }
+        top = max(m[0], m[1]);
     }
-    a = max_dpp<0xB1>(a);
-    const uint32_t any = __builtin_bit_cast(uint32_t, max_dpp<0xB1>(nan ? 1.f : 0.f)), bits = __builtin_bit_cast(uint32_t, a);
+    return max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));
+}
+
+// 16 elements as codes, and the biased exponent of the scale that they share with the neighbouring lane's 16: of the least power of two s
+// with a <= 7 s, where 7 is what still rounds to the largest code, 6, by no more than half a step.  The conversions do the division,
+// round to nearest even and take what is more than 5, infinities too, to 6.
+template <int DTYPE>
+static __device__ __forceinline__ uint32_t quantise_32(const Elements<DTYPE>& x, Elements<FA_FP4_E2M1>& y) {
+    constexpr uint32_t inf = DTYPE == FA_F32 ? 0x7F800000u : DTYPE == FA_BF16 ? 0x7F80u : 0x7C00u;
+    uint32_t top = largest_of_32<false>(x);
+    const bool nan = top > inf;
+    if (__builtin_expect(top >= inf, 0)) top = largest_of_32<true>(x);
+    const uint32_t bits = DTYPE == FA_F32 ? top : DTYPE == FA_BF16 ? top << 16 : __builtin_bit_cast(uint32_t, Elem<f16_tag>::to_float((uint16_t)top));
     const uint32_t biased = max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x600000u), 27);  // (no less than 2^-100)
-    const float factor = power_of_two(254 - biased);
-#pragma unroll
-    for (int t = 0; t < 16; ++t) f[t] = fminf(fmaxf(f[t] * factor, -6.f), 6.f);
-    return any ? 255 : biased;
+    y.set(x, power_of_two(biased));
+    return nan ? 255 : biased;
 }
 
 template <int D, int IN, int OUT>
@@ -189,16 +218,26 @@ __global__ void __launch_bounds__(256) fa_cache_write_kernel(Rows k, Rows v, Cac
         char* to = static_cast<char*>(i ? c.v : c.k) + (slot * LANES + lane) * Elements<OUT>::BYTES;
         if constexpr (IN == OUT) {
             x[i].template store<true>(to);
+        } else if constexpr (OUT == FA_FP4_E2M1) {
+            Elements<OUT> y;
+            const uint32_t scale = quantise_32(x[i], y);
+            y.template store<true>(to);
+            // (four neighbours' together: one store for eight lanes, at d = 64 for a row's four)
+            int scales = (int)(scale << (8 * (lane / 2 % 4)));
+            scales |= __builtin_amdgcn_mov_dpp(scales, 0x4E, 0xF, 0xF, true);
+            uint8_t* const at = static_cast<uint8_t*>(i ? c.v_scales : c.k_scales) + slot * (D / 32);
+            if constexpr (D == 64) {
+                if (lane == 0) *reinterpret_cast<uint16_t*>(at) = (uint16_t)scales;
+            } else {
+                scales |= __builtin_amdgcn_mov_dpp(scales, 0x141, 0xF, 0xF, true);  // row_half_mirror
+                if (lane % 8 == 0) *reinterpret_cast<int*>(at + lane / 2) = scales;
+            }
         } else {
             float f[16];
             x[i].get(f);
             if constexpr (OUT == FA_FP8_E4M3) {
                 const float scale = quantise<LANES>(f);
                 if (lane == 0) static_cast<float*>(i ? c.v_scales : c.k_scales)[slot] = scale;
-            }
-            if constexpr (OUT == FA_FP4_E2M1) {
-                const uint32_t scale = quantise_32(f);
-                if (lane % 2 == 0) static_cast<uint8_t*>(i ? c.v_scales : c.k_scales)[slot * (D / 32) + lane / 2] = (uint8_t)scale;
             }
             Elements<OUT> y;
             y.set(f);

@@ -56,6 +56,9 @@ def test_write(dense, B, H_kv, T, d, page, max_pages):
     border = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], device="cuda")
     v[0, -1, -1, :32] = torch.cat((border, -border, border / 2, -border / 4))
     v[0, -1, -1, 32:64] = 3.5
+    if dense == "f16":  # multiples of the smallest number there is
+        k[0, -1, -1, :32] = torch.arange(32, device="cuda") * 2.0 ** -24
+        k[0, -1, -1, 32:64] = -2.0 ** -24
     for n in (None, counts):
         have = [t.clone() for t in cache]
         got = binding.fa_cache_write(k, v, have[0], have[1], table.cuda(), lens.cuda(), counts=None if n is None else n.cuda(), k_scales=have[2], v_scales=have[3])
