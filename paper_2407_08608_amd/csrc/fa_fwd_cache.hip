@@ -443,8 +443,10 @@ struct CachedShape {
     static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
     static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 2 * 4 + NW * 4;
     static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
-    // workgroups (of four waves) to a CU, by registers
-    static constexpr int WAVES = SHARED ? (D == 64 ? 3 : D == 128 ? 2 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
+    // workgroups (of four waves) to a CU, by registers.  e2m1 with 16 columns takes few enough for more, where a wave has one tile ahead and
+    // not two: us, two to a SIMD and two tiles ahead / so, in teams, 32 x 500 to 4096 keys of 8 heads d = 64 22.5 / 19.5, d = 128 27.4 / 25.4,
+    // 64 sequences d = 128 45.7 / 40.8; but eight waves that have a whole sequence 26.1 / 26.4
+    static constexpr int WAVES = HELD == kCodes4 && !SHARED && COLS == 16 && D < 256 ? (D == 64 ? 4 : NW == 4 ? 3 : 2) : SHARED ? (D == 64 ? 3 : D == 128 ? 2 : 1) : COLS == 16 || (RT == 1 && D < 256) ? 2 : 1;
     static_assert(LDS <= 163840);
     static constexpr int BY_LDS = 163840 / LDS, PER_CU = BY_LDS < WAVES ? BY_LDS : WAVES;
 };
@@ -638,7 +640,7 @@ fa_fwd_cache_kernel(CachedArgs a) {
     constexpr bool UNITS = FOUR && std::is_same_v<Tag, f16_tag>;
     using Half = Rows4<D, 16>;
     using Keys = std::conditional_t<COLS == 16 || SHARED, Half, Rows4<D, 32>>;
-    constexpr int SETS = FOUR && COLS == 16 && D < 256 ? 2 : 1;  // (where two fit the registers)
+    constexpr int SETS = FOUR && COLS == 16 && D == 128 && NW == 8 ? 2 : 1;
     constexpr int KEY_TILES = COLS == 16 && !SHARED ? 2 : 1;
     Keys keys[SETS][KEY_TILES];
     Half values[SETS][SHARED ? 1 : 2];
@@ -1238,6 +1240,12 @@ constexpr int kAlone = 4608;
 template <typename Form>
 static bool whole_sequences(double workgroups, int max_len) {
     constexpr bool shared = Form::FORM == kShareKeys;
+    if constexpr (Form::HELD == kCodes4 && Form::COLS == 16 && Form::D < 256) {
+        // A key takes half of what it takes in e4m3, and there are more teams.  us, whole / teams, lengths spread as above: d = 64 128 2048
+        // 13.7 / 14.5, 512 4096 33.3 / 31.1;  d = 128 128 2048 16.8 / 16.5, 256 4096 26.4 / 25.4, 512 4096 43.7 / 40.8
+        const double limit = 8 * workgroups + 256 > 512 ? 8 * workgroups + 256 : 512;
+        return max_len <= kAlone * 3 / 4 && max_len * (Form::D == 64 ? 1.1 : 1.25) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
+    }
     constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
                      d256 = Form::COLS == 16 ? (Form::CODES ? 1.5 : 2.0) : shared ? 2.0 : 1.25;
     if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return max_len <= kAlone;
