@@ -382,7 +382,7 @@ struct Rows4 {
         }
         top = (int)Matrix<bf16_tag, D, ROWS>::max_parts((float)top);
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) scale[c] = max(scale[c] - top + 127, 0);
+        for (int c = 0; c < CHUNKS; ++c) scale[c] = min(max(scale[c] - top + 127, 0), 254);  // (of zeros it may be the larger)
         return __builtin_bit_cast(float, top == 255 ? 0x7FC00000 : top << 23);
     }
     // the eight elements of word U

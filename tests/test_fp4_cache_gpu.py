@@ -279,6 +279,28 @@ def test_scales_of_very_different_size(d, H, H_kv, T):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,H,H_kv,T", _FORMS)
+def test_scales_of_zeros_are_any(dtype, d, H, H_kv, T):
+    """A group of zeros, of either sign, is zero whatever its scale, and has no influence on the other groups' values"""
+    c = Case(700 + T, dtype, 2, H, H_kv, T, d, 16, [200, 50])
+    groups = np.random.default_rng(T).random(c.host["k_scales"].shape) < 0.3
+    big = {}
+    for n in ("k", "v"):
+        zero = torch.from_numpy(groups).cuda()
+        codes = torch.where(zero.repeat_interleave(16, -1), 0x80, c.args[n + "_pages"])
+        c.args[n + "_pages"], c.host[n + "_pages"] = codes, codes.cpu().numpy()
+        low = torch.where(zero & (c.args[n + "_scales"] != 255), 27, c.args[n + "_scales"]).to(torch.uint8)
+        c.args[n + "_scales"], c.host[n + "_scales"] = low, low.cpu().numpy()
+        big[n] = low
+    want = c.run()
+    c.check(*want)
+    for scale in (0, 1, 254, 228, 255 - 127, 253):
+        kw = {n + "_scales": torch.where(torch.from_numpy(groups).cuda() & (big[n] != 255), scale, big[n]).to(torch.uint8) for n in ("k", "v")}
+        got = c.run(**kw)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), scale
+
+
 def test_rising_scores():
     # every tile of keys raises the maximum
     for dtype in ("bf16", "f16"):
