@@ -72,6 +72,22 @@ def test_extend(B, B_new, wide, page, n_pages, held, T):
         _same(again, (want[0], want[1]))  # (what was not there is still missing)
 
 
+@pytest.mark.parametrize("B,wide,page,n_pages,T", [(1, 8200, 16, 8200, 131072), (3, 2100, 16, 4096, 20000), (1100, 70, 16, 9000, 100), (1, 1025, 1, 1030, 1024),
+                                                   (2, 1030, 1, 2100, 1030)])
+def test_extend_by_prompts(B, wide, page, n_pages, T):
+    """Many entries of few sequences, between sequences that get one, none, or have their pages"""
+    g = np.random.default_rng(B)
+    table = np.full((B, wide), -1)
+    lens = g.integers(0, 4 * page, B)
+    for b in range(B):
+        table[b, :lens[b] // page + 2] = g.integers(0, n_pages // 2, lens[b] // page + 2)
+    table[g.random((B, wide)) < 0.05] = n_pages - 1
+    for counts in (None, np.where(g.random(B) < 0.5, g.integers(0, 3, B), T)):
+        want = pages_oracle.extend(table, lens, np.full(B, T) if counts is None else counts, None, page, n_pages)
+        got = binding.fa_cache_extend(_ints(table), _ints(lens), T, page, n_pages, counts=None if counts is None else _ints(counts))
+        _same(got, want)
+
+
 @pytest.mark.parametrize("B,B_new,wide,page,n_pages", _SIZES)
 @pytest.mark.parametrize("held", [False, True])
 def test_compact(B, B_new, wide, page, n_pages, held):
