@@ -306,21 +306,40 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
         last = (int)min(end, (long)pool.max_pages - 1);
         return count > 0 ? (int)(end - max((long)first - 1, (long)last)) : 0;
     };
-    // f(entries, how many, how many past the table) in order: a sequence's by its thread if no sequence has many, else one by each thread.
-    // us, by sequences / by entries: one prompt of 131072 tokens in pages of 16 2675 / 28.3, four of a quarter of it 731 / 28.5; the test
-    // that decides costs the others less than 1
-    auto walk = [&](auto&& f) __attribute__((always_inline)) {
+    auto none = [&](const int* entry, int n) __attribute__((always_inline)) {
+        int sum = 0;
+        for (int e = 0; e < n; ++e) sum += !pool.has(entry[e]);
+        return sum;
+    };
+    auto give = [&](int* entry, int n, int at, const int* list, int most) __attribute__((always_inline)) {
+        for (int e = 0; e < n; ++e) {
+            if (pool.has(entry[e])) continue;
+            entry[e] = at < most ? list[at] : -1;
+            ++at;
+        }
+    };
+    // Few entries of a sequence are seen to by its thread.  If any has many, or some past the table, all go one by one over the threads.  us,
+    // by sequences / by entries: one prompt of 131072 tokens in pages of 16 2675 / 28.6, four of a quarter of it 731 / 28.4
+    constexpr int kMany = 8192;
+    static_assert(kMany > kOwnEntries * kThreads);
+    int* mine = nullptr;
+    int n_mine = 0;
+    auto by_sequences = [&](int b0, int& all) __attribute__((always_inline)) {
+        const int b = b0 + tid;
+        int first = 0, last = -1, past = 0;
+        if (b < a.B) past = entries(b, first, last);
+        mine = a.table + (long)b * pool.max_pages + first;
+        n_mine = max(last - first + 1, 0);
+        return sum_before(n_mine <= kOwnEntries && past == 0 ? none(mine, n_mine) : kMany, all, s.sums);
+    };
+    int all_past = 0;
+    auto by_entries = [&](auto&& f) __attribute__((always_inline)) {
         for (int b0 = 0; b0 < a.B; b0 += kThreads) {
             const int b = b0 + tid;
-            int first = 0, last = -1, past = 0;
-            if (b < a.B) past = entries(b, first, last);
-            const int n = max(last - first + 1, 0);
-            if (!__syncthreads_or(n > kOwnEntries)) {
-                f(a.table + (long)b * pool.max_pages + first, n, past);
-                continue;
-            }
-            int all;
-            s.seen[tid] = sum_before(n, all, s.sums);
+            int first = 0, last = -1, all;
+            if (b < a.B) all_past += entries(b, first, last);
+            const int before = sum_before(max(last - first + 1, 0), all, s.sums);
+            s.seen[tid] = before;
             s.whole[tid] = first;
             __syncthreads();
             for (int i0 = 0; i0 < all; i0 += kThreads) {
@@ -328,22 +347,25 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
                 int row = 0;  // the last that begins with entry i or before
 #pragma unroll
                 for (int step = kThreads / 2; step > 0; step /= 2) row += s.seen[row + step] <= i ? step : 0;
-                f(a.table + (long)(b0 + row) * pool.max_pages + s.whole[row] + i - s.seen[row], i < all ? 1 : 0, i0 == 0 ? past : 0);
+                f(a.table + (long)(b0 + row) * pool.max_pages + s.whole[row] + i - s.seen[row], i < all ? 1 : 0);
             }
+            __syncthreads();
         }
     };
-    auto none = [&](const int* entry, int n) __attribute__((always_inline)) {
+    int wanted = 0, beyond = 0, at = 0;
+    bool any_many = false;
+    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        int all;
+        at = by_sequences(b0, all);
+        wanted += all % kMany;
+        any_many |= all >= kMany;
+    }
+    if (any_many) {
         int sum = 0;
-        for (int e = 0; e < n; ++e) sum += !pool.has(entry[e]);
-        return sum;
-    };
-    int wanted, beyond, mine = 0, mine_past = 0;
-    walk([&](const int* entry, int n, int past) __attribute__((always_inline)) {
-        mine += none(entry, n);
-        mine_past += past;
-    });
-    sum_before(mine, wanted, s.sums);
-    sum_before(mine_past, beyond, s.sums);
+        by_entries([&](const int* entry, int n) __attribute__((always_inline)) { sum += none(entry, n); });
+        sum_before(sum, wanted, s.sums);
+        sum_before(all_past, beyond, s.sums);
+    }
     if (wanted == 0) {  // (as in most steps)
         if (tid == 0) *a.missing = beyond;
         return;
@@ -363,15 +385,23 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
     }
     const int most = min(found, asked);
     int before = 0;
-    walk([&](int* entry, int n, int) __attribute__((always_inline)) {
-        int all, at = before + sum_before(none(entry, n), all, s.sums);
-        before += all;
-        for (int e = 0; e < n; ++e) {
-            if (pool.has(entry[e])) continue;
-            entry[e] = at < most ? list[at] : -1;
-            ++at;
+    if (any_many) {
+        by_entries([&](int* entry, int n) __attribute__((always_inline)) {
+            int all;
+            const int from = before + sum_before(none(entry, n), all, s.sums);
+            before += all;
+            give(entry, n, from, list, most);
+        });
+    } else {
+        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+            if (a.B > kThreads) {
+                int all;
+                at = before + by_sequences(b0, all);
+                before += all;
+            }
+            give(mine, n_mine, at, list, most);
         }
-    });
+    }
     if (tid == 0) *a.missing = max(wanted - found, 0) + beyond;
 }
 

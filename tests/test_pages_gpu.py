@@ -73,19 +73,27 @@ def test_extend(B, B_new, wide, page, n_pages, held, T):
 
 
 @pytest.mark.parametrize("B,wide,page,n_pages,T", [(1, 8200, 16, 8200, 131072), (3, 2100, 16, 4096, 20000), (1100, 70, 16, 9000, 100), (1, 1025, 1, 1030, 1024),
-                                                   (2, 1030, 1, 2100, 1030)])
+                                                   (2, 1030, 1, 2100, 1030), (2050, 4, 16, 9000, 16)])
 def test_extend_by_prompts(B, wide, page, n_pages, T):
     """Many entries of few sequences, between sequences that get one, none, or have their pages"""
     g = np.random.default_rng(B)
     table = np.full((B, wide), -1)
     lens = g.integers(0, 4 * page, B)
     for b in range(B):
-        table[b, :lens[b] // page + 2] = g.integers(0, n_pages // 2, lens[b] // page + 2)
+        table[b, :lens[b] // page + 1] = g.integers(0, n_pages // 2, lens[b] // page + 1)
     table[g.random((B, wide)) < 0.05] = n_pages - 1
     for counts in (None, np.where(g.random(B) < 0.5, g.integers(0, 3, B), T)):
         want = pages_oracle.extend(table, lens, np.full(B, T) if counts is None else counts, None, page, n_pages)
         got = binding.fa_cache_extend(_ints(table), _ints(lens), T, page, n_pages, counts=None if counts is None else _ints(counts))
         _same(got, want)
+
+
+def test_extend_past_the_table():
+    """All of a sequence's places, and some, are past it; the others get theirs"""
+    table = np.full((3, 4), -1)
+    for lens in ([64, 0, 10], [60, 2 ** 31 - 1, 63], [64, 64, 100]):
+        for T in (1, 16, 100):
+            _same(binding.fa_cache_extend(_ints(table), _ints(lens), T, 16, 20), pages_oracle.extend(table, lens, [T] * 3, None, 16, 20))
 
 
 @pytest.mark.parametrize("B,B_new,wide,page,n_pages", _SIZES)
