@@ -11,7 +11,8 @@
 // around the library call, as ctypes does.
 // Host time of a call, us, ctypes and torch.empty / so: fa_fwd 8.9 / 5.9, fa_bwd 12.1 / 7.6,
 // fa_fp8_quant_hadamard 8.4 / 5.6, fa_fwd_fp8 9.2 / 6.1 (the launch itself is 2.4 to 3 of it); the calls on a cache check more:
-// fa_rope 13.2 / 6.2, fa_cache_write 12.8 / 5.4, fa_cache_read 10.4 / 4.4, fa_fwd_cache in one launch 16.0 / 6.6.
+// fa_rope 13.2 / 6.2, fa_cache_write 12.8 / 5.4, fa_cache_read 10.4 / 4.4, fa_fwd_cache in one launch 16.0 / 6.6,
+// fa_rope_axes 13.5 / 5.5, fa_cache_fork 16.6 / 5.8, fa_cache_extend 9.0 / 5.0, fa_cache_compact 14.4 / 5.8, fa_cache_copy 8.4 / 3.9.
 #include <Python.h>
 
 #include <ATen/ATen.h>

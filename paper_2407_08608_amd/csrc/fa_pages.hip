@@ -4,7 +4,12 @@
 // A page is free if no entry of the table names it and the caller does not hold it, so there are no counters that could go wrong: a
 // workgroup marks what is in use in a bitmap in the LDS, a window of the pool at a time, and a sum over its words gives the free pages
 // in ascending order.  What needs one gets them in its own order, so the result does not depend on the order of any atomic.  This is a
-// few kilobytes and a chain of some six dependent reads of memory: latency decides.  The copies move whole pages, and HBM decides.
+// few kilobytes and a chain of some six dependent reads of memory: latency decides, and for wide tables what one workgroup reads in a
+// time.  The copies move whole pages, and HBM decides.
+//
+// Measured, kernels alone, us: fork 16 rows of 32 entries 7.7, 128 of 257 in 3130 pages 10.1; extend 2.4 where nothing is wanted, the 128 rows
+// 7.7, 256 of 2048 in 100 thousand pages 44, of 8192 147; compact 4 rows 8.1, 64 of 128 in 7677 pages 16.7; copies of 115 MB to
+// 115 MB 42, 5.5 TB/s.
 #include "fa_device.h"
 #include "fa_launch.h"
 
