@@ -8,7 +8,7 @@
 // time.  The copies move whole pages, and HBM decides.
 //
 // Measured, kernels alone, us: fork 16 rows of 32 entries 7.7, 128 of 257 in 3130 pages 10.1; extend 2.4 where nothing is wanted, the 128 rows
-// 7.7, 256 of 2048 in 100 thousand pages 44, of 8192 147; compact 4 rows 8.1, 64 of 128 in 7677 pages 16.7; copies of 115 MB to
+// 7.7, 256 of 2048 in 100 thousand pages 41, of 8192 103; compact 4 rows 8.1, 64 of 128 in 7677 pages 16.7; copies of 115 MB to
 // 115 MB 42, 5.5 TB/s.
 #include "fa_device.h"
 #include "fa_launch.h"
@@ -83,9 +83,10 @@ static __device__ __forceinline__ int sum_before(int x, int& all, int* sums) {
     return before + upto - x;
 }
 
+// (a negative number less base is kWindow or more without a sign: base is 2^31 - kWindow at most)
 static __device__ __forceinline__ void mark(uint32_t* bits, int page, int base, int n) {
-    const unsigned at = (unsigned)(page - base);
-    if (page >= 0 && at < (unsigned)n) atomicOr(&bits[at >> 5], 1u << (at & 31));
+    const unsigned at = (unsigned)page - (unsigned)base;
+    if (at < (unsigned)n) atomicOr(&bits[at >> 5], 1u << (at & 31));
 }
 static __device__ __forceinline__ bool marked(const uint32_t* bits, int page, int base) { return bits[(page - base) >> 5] >> ((page - base) & 31) & 1; }
 
@@ -94,8 +95,11 @@ static __device__ __forceinline__ void clear(uint32_t* bits, int words) {
     __syncthreads();
 }
 
-// f(number, value) of n ints, 16 of a thread on their way at a time: one workgroup has nothing else to hide a read of memory behind
-template <typename F>
+// f(number, value) of n ints, 16 of a thread on their way at a time: one workgroup has nothing else to hide a read of memory behind.
+// With SKIPS four negative ones in a row may be left out: a look at each takes longer than the reads.  us, all looked at / so: fa_cache_extend
+// of 256 rows of 8192 entries, a thirteenth of them pages, 147 / 103,
+// of 2048 with a tenth 44 / 41
+template <bool SKIPS, typename F>
 static __device__ __forceinline__ void for_each_int(const int* p, int n, F&& f) {
     const int skip = min((int)(-(reinterpret_cast<uintptr_t>(p) / 4) & 3), n), whole = (n - skip) / 4;  // to where four ints are aligned
     const i32x4* const x = reinterpret_cast<const i32x4*>(p + skip);
@@ -109,7 +113,7 @@ static __device__ __forceinline__ void for_each_int(const int* p, int n, F&& f) 
         for (int j = 0; j < AHEAD; ++j) v[j] = x[min(i0 + j * kThreads, whole - 1)];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
-            if (i0 + j * kThreads < whole)
+            if (i0 + j * kThreads < whole && !(SKIPS && (v[j][0] & v[j][1] & v[j][2] & v[j][3]) < 0))
 #pragma unroll
                 for (int e = 0; e < 4; ++e) f(skip + 4 * (i0 + j * kThreads) + e, v[j][e]);
     }
@@ -118,12 +122,12 @@ static __device__ __forceinline__ void for_each_int(const int* p, int n, F&& f) 
 // What the caller holds, and all entries of a table
 static __device__ __forceinline__ void mark_held(uint32_t* bits, const Pool& pool, int base, int n) {
     if (pool.held)
-        for_each_int(pool.held + base, n, [&](int page, int held) {
+        for_each_int<false>(pool.held + base, n, [&](int page, int held) {
             if (held != 0) mark(bits, page, 0, n);
         });
 }
 static __device__ __forceinline__ void mark_table(uint32_t* bits, const int* table, int entries, int base, int n) {
-    for_each_int(table, entries, [&](int, int page) { mark(bits, page, base, n); });
+    for_each_int<true>(table, entries, [&](int, int page) { mark(bits, page, base, n); });
 }
 
 // The pages base .. base + n - 1 whose bit is `value` (and whose bit in `others` is not set) go to list[found ..] in ascending order, up to `most`
@@ -485,7 +489,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_compact_kernel(CompactArgs 
     }
     if (!a.renumbers) return;
     const int entries = a.B * pool.max_pages;
-    for_each_int(a.table, entries, [&](int i, int page) {
+    for_each_int<false>(a.table, entries, [&](int i, int page) {
         if (pool.has(page) && page >= threshold && !(pool.held && pool.held[page] != 0)) page = lists.to[page];
         a.new_table[i] = page;
     });
