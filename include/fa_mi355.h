@@ -349,7 +349,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const void* k_scales
  * and (src, dst)[i] says so.  So sequences branch, change places and end by their parents alone, and what no new sequence has is
  * free.  (Pages that the old table has behind a sequence's length are not taken over.)  Contents are to be copied before anything is
  * written to the new sequences.
- *   parents   : int32 [B_new];  new_table: int32 [B_new, max_pages];  new_lens, src, dst: int32 [B_new]
+ *   parents   : int32 [B_new];  new_table: int32 [B_new, max_pages];  new_lens, src, dst: int32 [B_new].  (new_table = block_table
+ *               or new_lens = lens: FA_ERR_SHAPE)
  *
  * fa_cache_extend: pages for the tokens that come next.  Entries of the places lens[b] .. lens[b] + counts[b] - 1 that are no page (-1, or
  * anything outside the pool) get a free one; block_table is changed in place.  Places past the table count as missing.

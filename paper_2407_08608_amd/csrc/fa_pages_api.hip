@@ -62,7 +62,8 @@ int fa_cache_fork(const int* block_table, const int* lens, const int* parents, c
     if (!block_table || !lens || !parents || !new_table || !new_lens || !src || !dst || !missing) return FA_ERR_NULL;
     int st = check_pool(B, n_pages, max_pages);
     if (st == FA_OK) st = check_pool(B_new, n_pages, max_pages);
-    if (st != FA_OK || page_size <= 0 || (long)max_pages * page_size > FA_CACHE_MAX_PLACES || new_table == block_table) return FA_ERR_SHAPE;
+    if (st != FA_OK || page_size <= 0 || (long)max_pages * page_size > FA_CACHE_MAX_PLACES || new_table == block_table || new_lens == lens)
+        return FA_ERR_SHAPE;  // (in place, some rows would be read after they have been written)
     for (const int* p : {block_table, lens, parents, held, (const int*)new_table, (const int*)new_lens, (const int*)src, (const int*)dst, (const int*)missing})
         if (!aligned_to(p, 4)) return FA_ERR_ALIGN;
     st = check_workspace(workspace, workspace_bytes, B_new, n_pages);

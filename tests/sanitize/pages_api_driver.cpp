@@ -37,12 +37,13 @@ int main() {
     EXPECT(fa_rope_axes(p, 0, p, 0, p, 0, p, 0, f, n, n, 0, 2, 4, 2, 16, 64, 64, 1.f, 0, FA_BF16, 0), FA_ERR_SHAPE);
     EXPECT(fa_rope_axes_bwd(p, 0, p, 0, p, 0, p, 0, f, odd, n, 3, 2, 4, 2, 16, 64, 64, 1.f, 0, FA_BF16, 0), FA_ERR_ALIGN);
     EXPECT(fa_rope_axes_bwd(p, 0, p, 0, p, 0, p, 0, f, n, 0, 3, 2, 4, 2, 16, 64, 64, 1.f, 0, FA_BF16, 0), FA_ERR_NULL);
-    EXPECT(fa_cache_fork(n, n, n, 0, m, n, n, n, n, p, 64, 3, 4, 16, 9, 5, 0), FA_OK);
-    EXPECT(fa_cache_fork(n, n, n, n, m, n, n, n, n, p, 63, 3, 4, 16, 9, 5, 0), FA_ERR_WORKSPACE);
-    EXPECT(fa_cache_fork(n, n, n, n, n, n, n, n, n, p, 64, 3, 4, 16, 9, 5, 0), FA_ERR_SHAPE);
-    EXPECT(fa_cache_fork(n, n, n, n, m, n, n, n, n, p, 64, 1, 0x7fffffff, 1, 0x7fffffff, 1, 0), FA_OK);
-    EXPECT(fa_cache_fork(n, n, n, n, m, n, n, n, n, p, 64, 1, 0x7fffffff, 1, 0x7fffffff, 2, 0), FA_ERR_SHAPE);
-    EXPECT(fa_cache_fork(n, n, n, n, m, n, n, n, n, p, 64, 1, 1, 0x7fffffff, 9, 0x7fffffff, 0), FA_ERR_SHAPE);
+    EXPECT(fa_cache_fork(n, n, n, 0, m, m, n, n, n, p, 64, 3, 4, 16, 9, 5, 0), FA_OK);
+    EXPECT(fa_cache_fork(n, n, n, n, m, m, n, n, n, p, 63, 3, 4, 16, 9, 5, 0), FA_ERR_WORKSPACE);
+    EXPECT(fa_cache_fork(n, n, n, n, n, m, n, n, n, p, 64, 3, 4, 16, 9, 5, 0), FA_ERR_SHAPE);
+    EXPECT(fa_cache_fork(n, n, n, n, m, n, n, n, n, p, 64, 3, 4, 16, 9, 5, 0), FA_ERR_SHAPE);
+    EXPECT(fa_cache_fork(n, n, n, n, m, m, n, n, n, p, 64, 1, 0x7fffffff, 1, 0x7fffffff, 1, 0), FA_OK);
+    EXPECT(fa_cache_fork(n, n, n, n, m, m, n, n, n, p, 64, 1, 0x7fffffff, 1, 0x7fffffff, 2, 0), FA_ERR_SHAPE);
+    EXPECT(fa_cache_fork(n, n, n, n, m, m, n, n, n, p, 64, 1, 1, 0x7fffffff, 9, 0x7fffffff, 0), FA_ERR_SHAPE);
     EXPECT(fa_cache_extend(n, n, 0, 0, n, p, 64, 3, 0x7fffffff / 3, 16, 9, 5, 0), FA_OK);
     EXPECT(fa_cache_extend(n, n, n, odd, n, p, 64, 3, 1, 16, 9, 5, 0), FA_ERR_ALIGN);
     EXPECT(fa_cache_extend(n, n, n, n, n, odd, 64, 3, 1, 16, 9, 5, 0), FA_ERR_ALIGN);

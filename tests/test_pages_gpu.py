@@ -276,6 +276,7 @@ def test_the_binding_refuses_what_does_not_fit():
                        (lambda: fork(t, lens, p, 0, 9), binding.FaError), (lambda: fork(t, lens, p, 16, 0), binding.FaError),
                        (lambda: fork(t, lens, p, 16, 9, held=lens), ValueError), (lambda: fork(t, lens, p, 16, 5000, workspace=small), binding.FaError),
                        (lambda: fork(t, lens, _ints([0, 1, 2]), 16, 9, new_table=t), binding.FaError),
+                       (lambda: fork(t, lens, _ints([0, 1, 2]), 16, 9, new_lens=lens), binding.FaError),
                        (lambda: fork(t, lens, p[:0], 16, 9), binding.FaError), (lambda: fork(t, lens, p, 16, 9, src=lens), ValueError),
                        (lambda: binding.fa_cache_extend(t, lens, 0, 16, 9), binding.FaError), (lambda: binding.fa_cache_extend(t, lens, 1, 16, 9, counts=p), ValueError),
                        (lambda: binding.fa_cache_extend(t.t(), lens, 1, 16, 9), ValueError), (lambda: binding.fa_cache_extend(t, lens, 2 ** 31 - 1, 16, 9), binding.FaError),

@@ -62,7 +62,7 @@ def test_copy_refuses_before_any_launch(kw, status):
 
 
 def _fork(**kw):
-    a = dict(table=P, lens=P, parents=P, held=P, new=2 * P, new_lens=P, src=P, dst=P, missing=P, ws=P, bytes=1 << 20, B=3, B_new=4, page=16, n_pages=9, max_pages=5)
+    a = dict(table=P, lens=P, parents=P, held=P, new=2 * P, new_lens=3 * P, src=P, dst=P, missing=P, ws=P, bytes=1 << 20, B=3, B_new=4, page=16, n_pages=9, max_pages=5)
     assert set(kw) <= set(a)
     a.update(kw)
     return binding.lib().fa_cache_fork(*a.values(), None)
@@ -87,7 +87,7 @@ def _compact(**kw):
                                (_compact, ("table", "new", "src", "dst", "top"))) for kw, s in
     [({p: None}, 1) for p in ptrs] + [({p: P + 2}, 5) for p in ptrs + ("held",)] +
     [(dict(B=0), 2), (dict(n_pages=0), 2), (dict(max_pages=0), 2), (dict(B=1 << 16, max_pages=1 << 15), 2), (dict(ws=None, n_pages=5000), 6), (dict(bytes=3, n_pages=5000), 6), (dict(ws=P + 8, n_pages=5000), 5)]
-] + [(_fork, dict(B_new=0), 2), (_fork, dict(B_new=-1), 2), (_fork, dict(page=0), 2), (_fork, dict(page=1 << 16, max_pages=1 << 15), 2), (_fork, dict(new=P), 2),
+] + [(_fork, dict(B_new=0), 2), (_fork, dict(B_new=-1), 2), (_fork, dict(page=0), 2), (_fork, dict(page=1 << 16, max_pages=1 << 15), 2), (_fork, dict(new=P), 2), (_fork, dict(new_lens=P), 2),
      (_fork, dict(B_new=1 << 16, max_pages=1 << 15), 2), (_extend, dict(T=0), 2), (_extend, dict(page=-1), 2), (_extend, dict(B=3, T=1 << 30), 2),
      (_extend, dict(counts=P + 1), 5), (_compact, dict(moves=0), 2), (_compact, dict(moves=-5), 2)])
 def test_pages_refuse_before_any_launch(call, kw, status):
