@@ -9,8 +9,8 @@
 // library product and 5 TB/s of a copy): the cache is read once per row group, straight into the LDS.  Measured with the join:
 // 32 sequences of 500 to 4096 keys, H = 32 on 8, bf16, T = 1: 268 MB in 51 us, 5.2 TB/s; 2 of up to 65536 keys, H = 16 on 2,
 // d = 256, codes: 129 MB in 33 us, of which some 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
-// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop; over e2m1 the first in 26 us
-// (2.7 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 43.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop; over e2m1 the first in 25 us
+// (2.9 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 44.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
 // refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
@@ -510,13 +510,20 @@ fa_fwd_cache_kernel(CachedArgs a) {
             total += __builtin_amdgcn_readlane(upto, 63);
         }
         shares = Shares(total * H_kv, a.teams);
-        // Where a share of at most one step more lets each team stay with one sequence and head, it does: no second start
-        uint32_t parts = 0, parts_upto = 0;
+        // Where a share of at most MORE steps more lets each team stay with one sequence and head, it does: no second start.  With e2m1 a
+        // step is short beside a start: us, MORE 1 / 2, T = 1, 8 heads, d = 128 32 x 500 to 4096 keys 27.1 / 24.7, to 8192 38.5 / 36.5, 64 x 500 to
+        // 4096 42.4 / 42.8; 13 x 2000 to 9000, d = 256 48.6 / 46.1; 24 x 4000 to 9000, 4 heads of 32 rows 37.5 / 33.4; 3 is as 2, or 1 % more
+        constexpr uint32_t MORE = FOUR ? 2 : 1;
+        uint32_t parts = 0, parts_upto = 0, used = 0;
         if (a.B <= 64) {
-            parts = (n + shares.each) / (shares.each + 1);
-            parts_upto = sum_upto(parts, lane);
+#pragma unroll 1
+            for (uint32_t most = shares.each + 1;; ++most) {
+                parts = (n + most - 1) / most;
+                parts_upto = sum_upto(parts, lane);
+                used = __builtin_amdgcn_readlane(parts_upto, 63) * H_kv;
+                if (MORE == 1 || used <= (uint32_t)a.teams || most == shares.each + MORE) break;
+            }
         }
-        const uint32_t used = __builtin_amdgcn_readlane(parts_upto, 63) * H_kv;
         int i;
         if (a.B <= 64 && used <= (uint32_t)a.teams) {
             if ((uint32_t)team >= used) return;
@@ -637,11 +644,12 @@ fa_fwd_cache_kernel(CachedArgs a) {
             }
     };
     // e2m1: tiles on their way in registers, SETS of them.  kDivideKeys: K and V of the wave's own; kShareKeys: 16 rows of the tile that all
-    // share, of K in waves 0 and 1 and of V in waves 2 and 3
+    // share, of K in waves 0 and 1 and of V in waves 2 and 3 (two tiles ahead / one, bf16: 8 trees of 32 tokens, 16 rows to each, over up to 16384
+    // keys 78.8 / 82.9 us, d = 256 70.1 / 72.8; fp16 within 1 %)
     constexpr bool UNITS = FOUR && std::is_same_v<Tag, f16_tag>;
     using Half = Rows4<D, 16>;
     using Keys = std::conditional_t<COLS == 16 || SHARED, Half, Rows4<D, 32>>;
-    constexpr int SETS = FOUR && COLS == 16 && D == 128 && NW == 8 ? 2 : 1;
+    constexpr int SETS = FOUR && (SHARED || (COLS == 16 && D == 128 && NW == 8)) ? 2 : 1;
     constexpr int KEY_TILES = COLS == 16 && !SHARED ? 2 : 1;
     Keys keys[SETS][KEY_TILES];
     Half values[SETS][SHARED ? 1 : 2];
@@ -707,7 +715,8 @@ fa_fwd_cache_kernel(CachedArgs a) {
             }
         }
     };
-    TileRows rows4[2];  // of the tile that is worked on next and the one after
+    TileRows rows4[2];  // of the tiles on their way
+    int bad4 = 0;       // kShareKeys: of the tile that is worked on next
     int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
     i32x4 qreg[RT][QS];
 #pragma unroll
@@ -734,14 +743,16 @@ fa_fwd_cache_kernel(CachedArgs a) {
             rows4[0] = locate(0);
             fetch_keys(rows4[0], first);
             fetch_values(rows4[0], first);
-            if constexpr (SETS == 2 || SHARED) rows4[1] = locate(1);
             if constexpr (SETS == 2) {
+                rows4[1] = locate(1);
                 fetch_keys(rows4[1], std::integral_constant<int, SETS - 1>{});
                 fetch_values(rows4[1], std::integral_constant<int, SETS - 1>{});
             }
             if constexpr (SHARED) {
                 put(0, rows4[0], first, 0);
-                fetch_values(rows4[1], first);
+                bad4 = rows4[0].bad();
+                rows4[0] = locate(2);
+                fetch_values(rows4[0], first);
             }
         } else if constexpr (SHARED) {
 #pragma unroll
@@ -970,7 +981,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
     };
     if constexpr (FOUR && SHARED) {
         // Tile i + 1 goes where tile i - 1 was, which all waves have left when they meet in tile i
-        constexpr std::integral_constant<int, 0> set;
         for (int i0 = 0; i0 < mine; i0 += STG)
             static_for<STG>([&](auto stage) __attribute__((always_inline)) {
                 constexpr int st = decltype(stage)::value;
@@ -978,11 +988,12 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 const int i = i0 + st;
                 if (i >= mine) return;
                 barrier();
-                const int bad = rows4[0].bad();
-                put(i + 1, rows4[1], set, (st ^ 1) * Shape::STAGE_B);
-                rows4[0] = rows4[1];
-                rows4[1] = locate(i + 2);
-                fetch_values(rows4[1], set);
+                constexpr std::integral_constant<int, st ^ 1> next;
+                const int bad = bad4;
+                put(i + 1, rows4[st ^ 1], next, (st ^ 1) * Shape::STAGE_B);
+                bad4 = rows4[st ^ 1].bad();
+                rows4[st ^ 1] = locate(i + 3);
+                fetch_values(rows4[st ^ 1], next);
                 __builtin_amdgcn_sched_barrier(0);
                 work(tile, keys[0], std::integral_constant<int, st * Shape::STAGE_B>{}, key0 + 32 * i, bad, [] {}, [] {}, [] {});
             });
