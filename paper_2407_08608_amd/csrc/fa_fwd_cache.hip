@@ -9,8 +9,8 @@
 // library product and 5 TB/s of a copy): the cache is read once per row group, straight into the LDS.  Measured with the join:
 // 32 sequences of 500 to 4096 keys, H = 32 on 8, bf16, T = 1: 268 MB in 51 us, 5.2 TB/s; 2 of up to 65536 keys, H = 16 on 2,
 // d = 256, codes: 129 MB in 33 us, of which some 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
-// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop; over e2m1 the first in 25 us
-// (2.9 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 44.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop; over e2m1 the first in 24 us
+// (3.0 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 43.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
 // refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
@@ -514,16 +514,16 @@ fa_fwd_cache_kernel(CachedArgs a) {
         // step is short beside a start: us, MORE 1 / 2, T = 1, 8 heads, d = 128 32 x 500 to 4096 keys 27.1 / 24.7, to 8192 38.5 / 36.5, 64 x 500 to
         // 4096 42.4 / 42.8; 13 x 2000 to 9000, d = 256 48.6 / 46.1; 24 x 4000 to 9000, 4 heads of 32 rows 37.5 / 33.4; 3 is as 2, or 1 % more
         constexpr uint32_t MORE = FOUR ? 2 : 1;
-        uint32_t parts = 0, parts_upto = 0, used = 0;
+        uint32_t parts = 0, parts_upto = 0;
         if (a.B <= 64) {
 #pragma unroll 1
-            for (uint32_t most = shares.each + 1;; ++most) {
-                parts = (n + most - 1) / most;
+            for (uint32_t more = 1;; ++more) {
+                parts = (n + shares.each + more - 1) / (shares.each + more);
                 parts_upto = sum_upto(parts, lane);
-                used = __builtin_amdgcn_readlane(parts_upto, 63) * H_kv;
-                if (MORE == 1 || used <= (uint32_t)a.teams || most == shares.each + MORE) break;
+                if (more == MORE || __builtin_amdgcn_readlane(parts_upto, 63) * H_kv <= (uint32_t)a.teams) break;
             }
         }
+        const uint32_t used = __builtin_amdgcn_readlane(parts_upto, 63) * H_kv;
         int i;
         if (a.B <= 64 && used <= (uint32_t)a.teams) {
             if ((uint32_t)team >= used) return;
