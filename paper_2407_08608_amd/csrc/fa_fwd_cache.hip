@@ -26,7 +26,7 @@
 //     no weight depends on a scale of another key, seen or not, and sixteen bits of each reach the product.
 //   - e2m1: codes and scales come to registers up to two tiles ahead (Rows4).  Their values are bf16 numbers whatever the scales, so no
 //     scale is left that a weight would have to bear.  V's go to the LDS as a tile of a bf16 cache; K's too where waves share them,
-//     else they become operands where they are, a word of codes each.  P goes to V as two bf16 numbers with fp16 Q, as with e4m3.
+//     else they become operands where they are, a word of codes each.  P goes to V as two bf16 numbers, as with e4m3.
 //     What this costs is instructions: at d = 128 a tile of 32 keys and 16 columns is 64 conversions of 7 cycles of some 330 instructions
 //     in all; it takes a SIMD 0.56 us, from the caches as from memory.  (The matrix instructions that take a power of two for 32 elements
 //     themselves would spare K's half of the conversions; but they add up products in some 17 bits below the largest: errors of 2^-11 of it
@@ -471,7 +471,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // With codes always: one bf16 number would be eight times as coarse as the fp16 number that a factor common to all keys allows, and
     // no common factor is right where a key of a large scale weighs little, or nothing (8 trees of 32 tokens, 8 heads: 53.0 us, with
     // fp16 and such a factor 51.3; 64 x 500 to 4096 keys, T = 1, d = 64: 26.1 and 27.8).
-    constexpr bool TWO_PARTS = COLS == 16 || CODES || (FOUR && std::is_same_v<Tag, f16_tag>);
+    // With e2m1 always too: one bf16 number beside Q of bf16 is 1.3 times the error of the output's rounding alone, and a third of all outputs
+    // another number (us, one / two, bf16: 8 trees of 32, 128 rows, 5000 to 8192 keys d = 64 31.2 / 33.8, d = 128 38.5 / 41.8, d = 256
+    // 61 / 69; 24 x 4000 to 9000 of 32 rows d = 128 34.5 / 39.1; 16 x 3000 to 6000 of 52 rows d = 128 32.4 / 36.0).
+    constexpr bool TWO_PARTS = COLS == 16 || CODES || FOUR;
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
