@@ -404,9 +404,8 @@ int fa_cache_copy(void* k_pages, void* v_pages, void* k_scales, void* v_scales, 
  * the sums are fp32.  For their product with V the probabilities are rounded to the 16-bit type of the cache, to two numbers of it
  * (a value and what that leaves out) with up to 16 rows (H / H_kv * T) to a key/value head; with FA_FP8_E4M3 the probabilities
  * times V's scales, which may have either sign, to two bf16 numbers always.  With FA_FP4_E2M1 V's values are
- * bf16 numbers, and the probabilities two of them.  K's are bf16 numbers too, or with fp16 Q fp16 numbers in units of the largest scale of the token
- * and head that has a code other than zero: what is 2^-24 of that and less counts as zero.  With p up to 2^8 for the largest of a row, sum p |v| and
- * p times V's scales have to stay within fp32.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One
+ * bf16 numbers, and the probabilities two of them; K's are bf16 numbers too, and fp16 Q two of them, exactly.  With p up to 2^8 for the
+ * largest of a row, sum p |v| and p times V's scales have to stay within fp32.  Nothing is accumulated with atomics: results are bit-for-bit repeatable.  One
  * launch, or two where sequences are divided.
  */
 #define FA_CACHE_MAX_TOKENS 256

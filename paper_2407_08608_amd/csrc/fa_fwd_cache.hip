@@ -26,7 +26,7 @@
 //     no weight depends on a scale of another key, seen or not, and sixteen bits of each reach the product.
 //   - e2m1: codes and scales come to registers up to two tiles ahead (Rows4).  Their values are bf16 numbers whatever the scales, so no
 //     scale is left that a weight would have to bear.  V's go to the LDS as a tile of a bf16 cache; K's too where waves share them,
-//     else they become operands where they are, a word of codes each.  P goes to V as two bf16 numbers, as with e4m3.
+//     else they become operands where they are, a word of codes each.  P goes to V as two bf16 numbers, as with e4m3; fp16 Q is two.
 //     What this costs is instructions: at d = 128 a tile of 32 keys and 16 columns is 64 conversions of 7 cycles of some 330 instructions
 //     in all; it takes a SIMD 0.56 us, from the caches as from memory.  (The matrix instructions that take a power of two for 32 elements
 //     themselves would spare K's half of the conversions; but they add up products in some 17 bits below the largest: errors of 2^-11 of it
@@ -131,6 +131,24 @@ static __device__ __forceinline__ i32x4 from_codes(int lo, int hi) {
         w[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
     }
     return w;
+}
+
+// Eight fp16 numbers as bf16 numbers and what these leave out, which is one exactly: 11 digits in 8 and at most 3 more, and bf16 has
+// fp16's smallest numbers as normal ones.  (Of an infinity or a NaN nothing is left out.)
+static __device__ __forceinline__ void split_f16(i32x4& x, i32x4& rest) {
+    using F = Elem<f16_tag>;
+    using G = Elem<bf16_tag>;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = (uint32_t)x[i];
+        const float lo = F::to_float((uint16_t)u), hi = F::to_float((uint16_t)(u >> 16));
+        const uint32_t w = (uint32_t)G::pack2(lo, hi);
+        float lo_rest = lo - G::to_float((uint16_t)w), hi_rest = hi - G::to_float((uint16_t)(w >> 16));
+        lo_rest = lo_rest == lo_rest ? lo_rest : 0.f;
+        hi_rest = hi_rest == hi_rest ? hi_rest : 0.f;
+        x[i] = (int)w;
+        rest[i] = (int)G::pack2(lo_rest, hi_rest);
+    }
 }
 
 // A code (its low four bits) over its scale's biased exponent
@@ -332,9 +350,7 @@ struct UniformRow {
 enum Held { kWords, kCodes8, kCodes4 };
 
 // ROWS (16, or 32) rows of e2m1 codes on their way from the pages: a lane has chunks of 8 WORDS elements of row lane % ROWS, and the bytes of
-// their scales.  A word becomes eight 16-bit elements.
-//   UNITS: fp16 does not have the range of the scales.  There the elements are in units of the row's largest scale (of codes that are not
-//   zero), which the score is multiplied by; what is 2^-24 of it and less is lost.  bf16 has: the elements are the values.
+// their scales.  A word becomes eight bf16 numbers.
 template <int D, int ROWS>
 struct Rows4 {
     static constexpr int ROWB = D / 2, PARTS = 64 / ROWS, WORDS = D == 64 && ROWS == 16 ? 2 : 4, CHUNKS = D / (8 * WORDS * PARTS);
@@ -371,43 +387,27 @@ struct Rows4 {
             scale[c] = 0;
         }
     }
-    // The row's unit; the scales become relative to it.  PARTS lanes have a row's chunks.
-    __device__ __forceinline__ float take_unit() {
-        int top = 1;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            int any = 0;
-#pragma unroll
-            for (int w = 0; w < WORDS; ++w) any |= code[c][w];
-            top = max(top, (any & 0x77777777) != 0 || scale[c] == 255 ? scale[c] : 1);
-        }
-        top = (int)Matrix<bf16_tag, D, ROWS>::max_parts((float)top);
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) scale[c] = min(max(scale[c] - top + 127, 0), 254);  // (of zeros it may be the larger)
-        return __builtin_bit_cast(float, top == 255 ? 0x7FC00000 : top << 23);
-    }
     // the eight elements of word U
-    template <int U, bool UNITS>
+    template <int U>
     __device__ __forceinline__ i32x4 operand() const {
         const float s = __builtin_bit_cast(float, scale[U / WORDS] << 23);
         const uint32_t w = (uint32_t)code[U / WORDS][U % WORDS];
         i32x4 y;
         static_for<4>([&](auto n) __attribute__((always_inline)) {
             constexpr int B = decltype(n)::value;
-            if constexpr (UNITS) y[B] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, B));
-            else y[B] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, B));
+            y[B] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, B));
         });
         return y;
     }
-    // All 16 rows as 16-bit elements into a tile.  `to`: the lane's place there for word 0 of row lane % 16; the others are an exclusive or
+    // All 16 rows as bf16 numbers into a tile.  `to`: the lane's place there for word 0 of row lane % 16; the others are an exclusive or
     // away, so 16 lanes of a write hit every bank once.
-    template <bool UNITS, int FLIP = 0, int OFFSET = 0>
+    template <int FLIP = 0, int OFFSET = 0>
     __device__ __forceinline__ void put(uint32_t to) const {
         static_assert(ROWS == 16);
         typedef i32x4 __attribute__((address_space(3))) * lds_vec_ptr;
         static_for<CHUNKS * WORDS>([&](auto n) __attribute__((always_inline)) {
             constexpr int u = decltype(n)::value;
-            *(lds_vec_ptr)(uintptr_t)((to ^ (uint32_t)((u % WORDS ^ FLIP) << 4)) + (OFFSET + u / WORDS * 256)) = operand<u, UNITS>();
+            *(lds_vec_ptr)(uintptr_t)((to ^ (uint32_t)((u % WORDS ^ FLIP) << 4)) + (OFFSET + u / WORDS * 256)) = operand<u>();
         });
     }
 };
@@ -439,11 +439,15 @@ struct CachedShape {
     static constexpr bool SHARED = FORM == kShareKeys;
     static constexpr int ROWS = COLS * RT * (SHARED ? NW : 1);  // of a workgroup
     static constexpr int STEP = SHARED && HELD == kCodes4 ? 64 : 32 * NW;  // keys of a step
-    static constexpr int SCALE_B = HELD == kWords ? 0 : 256;    // of a tile: 32 scales of K, 32 of V; e2m1: 32 units of K
+    static constexpr int SCALE_B = CODES ? 256 : 0;             // of a tile: 32 scales of K, 32 of V
     static constexpr int STAGE_B = (HELD == kCodes4 && !SHARED ? 1 : 2) * Tile::TILE_B + SCALE_B, STAGES_B = STG * STAGE_B * (SHARED ? 1 : NW);
     static constexpr int MERGE_COLS = (COLS == 16 || RT == 2) && D > 64 ? 128 : 64, MERGE_STRIDE = MERGE_COLS + 4;
     static constexpr int MERGE_B = NW * COLS * MERGE_STRIDE * 4, STATE_B = NW * COLS * RT * 2 * 4 + NW * 4;
-    static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + STATE_B;
+    // fp16 Q over e2m1 is two bf16 numbers (SPLIT).  What the first ones leave out is in the LDS where the registers are needed: us, in
+    // registers / so, 64 x 500 to 4096 keys d = 128 50.5 / 47.6, 2 x 50000 and more d = 256 36.7 / 31.6 (spills), 32 rows d = 128 41.9 / 41.5
+    static constexpr bool SPLIT = HELD == kCodes4 && std::is_same_v<Tag, f16_tag>, REST_IN_LDS = SPLIT && !SHARED && D >= 128;
+    static constexpr int REST_B = REST_IN_LDS ? RT * COLS * D * 2 : 0;
+    static constexpr int LDS = (STAGES_B > MERGE_B ? STAGES_B : MERGE_B) + REST_B + STATE_B;
     // workgroups (of four waves) to a CU, by registers.  e2m1 with 16 columns takes few enough for more, where a wave has one tile ahead and
     // not two: us, two to a SIMD and two tiles ahead / so, in teams, 32 x 500 to 4096 keys of 8 heads d = 64 22.5 / 19.5, d = 128 27.4 / 25.4,
     // 64 sequences d = 128 45.7 / 40.8; but eight waves that have a whole sequence 26.1 / 26.4
@@ -463,7 +467,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
     using PM = typename Tile::PM;
     using PE = Elem<typename Tile::PE>;
     using E = Elem<Tag>;
-    using MQ = Matrix<Tag, D, COLS>;  // of the product with Q
     constexpr int NS = M::NS, NT = M::NT, NI = Tile::NI, X = CODES ? 1 : 0, ACC = sizeof(typename M::Acc) / 4;
     constexpr bool ACCUMULATION = Shape::WAVES == 1;  // more than 256 registers: accumulators in the half for matrix results
     // Few rows leave the matrix pipes idle: P goes in as its rounded value and what that leaves out, so that its rounding does not
@@ -476,6 +479,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // 61 / 69; 24 x 4000 to 9000 of 32 rows d = 128 34.5 / 39.1; 16 x 3000 to 6000 of 52 rows d = 128 32.4 / 36.0).
     constexpr bool TWO_PARTS = COLS == 16 || CODES || FOUR;
     constexpr int QS = D / (8 * M::PARTS);  // steps of the scores' contraction
+    // fp16 does not have the range of e2m1's scales, and one bf16 number not the digits of fp16's Q: there Q is two, exactly.  us, K in fp16
+    // under a unit of each row, which lost groups of 2^-24 of the largest / so: 32 x 500 to 4096 keys, T = 1 d = 64 21.8 / 20.8, d = 128
+    // 27.0 / 26.4; 2 x 50000 and more, d = 256 30.8 / 31.6; 24 x 4000 to 9000 of 32 rows d = 128 38.9 / 41.5; 8 trees of 32, 128 rows, d = 128 45.3 / 46.7
+    constexpr bool SPLIT = Shape::SPLIT, REST_IN_LDS = Shape::REST_IN_LDS;
     extern __shared__ __align__(256) char lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int col = lane % COLS, part = lane / COLS, kw = SHARED ? 0 : wave, rw = SHARED ? wave : 0;
@@ -649,7 +656,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
     // e2m1: tiles on their way in registers, SETS of them.  kDivideKeys: K and V of the wave's own; kShareKeys: 16 rows of the tile that all
     // share, of K in waves 0 and 1 and of V in waves 2 and 3 (two tiles ahead / one, bf16: 8 trees of 32 tokens, 16 rows to each, over up to 16384
     // keys 78.8 / 82.9 us, d = 256 70.1 / 72.8; fp16 within 1 %)
-    constexpr bool UNITS = FOUR && std::is_same_v<Tag, f16_tag>;
     using Half = Rows4<D, 16>;
     using Keys = std::conditional_t<COLS == 16 || SHARED, Half, Rows4<D, 32>>;
     constexpr int SETS = FOUR && (SHARED || (COLS == 16 && D == 128 && NW == 8)) ? 2 : 1;
@@ -700,28 +706,22 @@ fa_fwd_cache_kernel(CachedArgs a) {
             const bool part_of_it = there < 32 || bad != 0;
             if constexpr (SHARED) {
                 if (part_of_it && !((lane & 15) + 16 * (wave & 1) < there && !(bad >> (wave & 1) & 1))) v[0].clear();
-                if (UNITS && wave < 2) {
-                    typedef float __attribute__((address_space(3))) * lds_float_ptr;
-                    const float unit = v[0].take_unit();
-                    if (lane < 16) *(lds_float_ptr)(uintptr_t)(tile.base + offset + 2 * Tile::TILE_B + 4 * (16 * (wave & 1) + lane)) = unit;
-                    v[0].template put<UNITS>(put_at + offset);
-                } else {
-                    v[0].template put<false>(put_at + offset);
-                }
+                v[0].template put<>(put_at + offset);
             } else {
                 if (part_of_it) {
                     if (!((lane & 15) < there && !(bad & 1))) v[0].clear();
                     if (!((lane & 15) + 16 < there && !(bad & 2))) v[SHARED ? 0 : 1].clear();
                 }
-                v[0].template put<false>(put_at + offset);
-                v[SHARED ? 0 : 1].template put<false, Tile::swizzle(16), 16 * Tile::ROWB>(put_at + offset);
+                v[0].template put<>(put_at + offset);
+                v[SHARED ? 0 : 1].template put<Tile::swizzle(16), 16 * Tile::ROWB>(put_at + offset);
             }
         }
     };
     TileRows rows4[2];  // of the tiles on their way
     int bad4 = 0;       // kShareKeys: of the tile that is worked on next
     int t[RT];  // the token of the lane's rows (clamped: rows past the end compute a copy of the last, never stored)
-    i32x4 qreg[RT][QS];
+    i32x4 qreg[RT][QS], qrest[RT][SPLIT && !REST_IN_LDS ? QS : 1];
+    const uint32_t rest_at = lds_address(lds) + (Shape::LDS - Shape::STATE_B - Shape::REST_B) + lane * 16;  // + 1 KiB (x QS + u)
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int row = min(((rg * RW + rw) * RT + x) * COLS + col, max(n_rows - 1, 0)), g = row / per;
@@ -739,7 +739,19 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
-        for (int u = 0; u < QS; ++u) asm volatile("" : "+v"(qreg[x][u]));
+        for (int u = 0; u < QS; ++u) {
+            if constexpr (REST_IN_LDS) {  // (all waves have the same rows: each puts its share)
+                typedef i32x4 __attribute__((address_space(3))) * lds_vec_ptr;
+                i32x4 rest;
+                split_f16(qreg[x][u], rest);
+                if (u % NW == wave) *(lds_vec_ptr)(uintptr_t)(rest_at + 1024 * (x * QS + u)) = rest;
+            } else if constexpr (SPLIT) {
+                split_f16(qreg[x][u], qrest[x][u]);
+                asm volatile("" : "+v"(qrest[x][u]));
+            }
+            asm volatile("" : "+v"(qreg[x][u]));
+        }
+    if constexpr (REST_IN_LDS) barrier();
     if (mine > 0) {
         if constexpr (FOUR) {
             constexpr std::integral_constant<int, 0> first;
@@ -808,21 +820,22 @@ fa_fwd_cache_kernel(CachedArgs a) {
 #pragma unroll
                     for (int kt = 0; kt < M::TILES; ++kt) y[x][kt] = typename M::Acc{};
                 if constexpr (FOUR && !SHARED) {
-                    if constexpr (UNITS) {
-                        typedef float __attribute__((address_space(3))) * lds_float_ptr;
-#pragma unroll
-                        for (int kt = 0; kt < M::TILES; ++kt) {
-                            const float unit = codes[kt].take_unit();
-                            if (part == 0) *(lds_float_ptr)(uintptr_t)(at.base + kScales + 4 * (16 * kt + col)) = unit;
-                        }
-                    }
                     static_for<QS>([&](auto n) __attribute__((always_inline)) {
                         constexpr int u = decltype(n)::value;
+                        i32x4 rest[RT];
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) {
+                            if constexpr (REST_IN_LDS) rest[x] = lds_load_16B(rest_at + 1024 * (x * QS + u));
+                            else if constexpr (SPLIT) rest[x] = qrest[x][u];
+                        }
                         static_for<M::TILES>([&](auto tile_no) __attribute__((always_inline)) {
                             constexpr int kt = decltype(tile_no)::value;
-                            const i32x4 w = codes[kt].template operand<u, UNITS>();
+                            const i32x4 w = codes[kt].template operand<u>();
 #pragma unroll
-                            for (int x = 0; x < RT; ++x) y[x][kt] = MQ::mma(w, qreg[x][u], y[x][kt]);
+                            for (int x = 0; x < RT; ++x) {
+                                y[x][kt] = M::mma(w, qreg[x][u], y[x][kt]);
+                                if constexpr (SPLIT) y[x][kt] = M::mma(w, rest[x], y[x][kt]);
+                            }
                         });
                     });
                 }
@@ -846,7 +859,10 @@ fa_fwd_cache_kernel(CachedArgs a) {
                             for (int x = 0; x < RT; ++x) y[x][kt] = M::mma(hi, qreg[x][2 * k + 1], y[x][kt]);
                         } else {
 #pragma unroll
-                            for (int x = 0; x < RT; ++x) y[x][kt] = MQ::mma(w, qreg[x][k], y[x][kt]);
+                            for (int x = 0; x < RT; ++x) {
+                                y[x][kt] = M::mma(w, qreg[x][k], y[x][kt]);
+                                if constexpr (SPLIT) y[x][kt] = M::mma(w, qrest[x][k], y[x][kt]);
+                            }
                         }
                     });
                 });
@@ -854,17 +870,6 @@ fa_fwd_cache_kernel(CachedArgs a) {
                 for (int x = 0; x < RT; ++x)
 #pragma unroll
                     for (int r = 0; r < NS; ++r) s[x][r] = y[x][r / ACC][r % ACC];
-            }
-            if constexpr (UNITS) {
-                asm volatile("" ::: "memory");  // (a wave's own: in order)
-#pragma unroll
-                for (int g = 0; g < NS / 4; ++g) {
-                    const f32x4 unit = lds_load_4f(at.base + kScales + 4 * (M::bit(4 * g) + (part << M::SHIFT)));
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int x = 0; x < RT; ++x) s[x][4 * g + r] *= unit[r];
-                }
             }
             float vscale[NS];
             if constexpr (CODES) {

@@ -1,9 +1,10 @@
 """What attention over a 4-bit cache keeps of its operands, whatever the types and the number of rows: probabilities have 16 bits in their product
-with V."""
+with V, and a product of Q and K is exact, however far a row's scales are apart."""
 import numpy as np
 import pytest
+import torch
 
-from test_fp4_cache_gpu import Case
+from test_fp4_cache_gpu import Case, _FORMS
 from test_fwd_cache_gpu import _random_tree
 
 pytestmark = pytest.mark.gpu
@@ -19,3 +20,33 @@ def test_probabilities_have_16_bits_with_many_rows(d, H, H_kv, T, max_len):
     c = Case(800 + T + d, "bf16", 2, H, H_kv, T, d, 16, [150, 333], tree=_random_tree(T, 2, T))
     c.rows = 16
     c.check(*c.run(max_len=max_len))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,H,H_kv,T", _FORMS)
+@pytest.mark.parametrize("max_len", [0, 1 << 20])
+def test_a_large_group_that_meets_zeros(dtype, d, H, H_kv, T, max_len):
+    """One group of each key has a scale 2^40 times and more the others', and Q zeros there: the score is that of the others"""
+    c = Case(900 + T + d, dtype, 2, H, H_kv, T, d, 16, [150, 70], tree=_random_tree(T, 2, T))
+    scales = c.host["k_scales"]
+    scales[..., 1] = np.where(scales[..., 1] == 255, 255, np.minimum(scales[..., 1].astype(int) + 44, 254))
+    c.args["k_scales"] = torch.from_numpy(scales).cuda()
+    c.q[..., 32:64] = 0
+    c.check(*c.run(max_len=max_len))
+
+
+@pytest.mark.parametrize("d,H,H_kv,T", _FORMS)
+def test_the_smallest_and_largest_queries(d, H, H_kv, T):
+    # multiples of fp16's smallest number, most of them subnormal, and numbers up to its largest, in groups whose keys make up for it
+    c = Case(950 + T + d, "f16", 2, H, H_kv, T, d, 16, [150, 70], tree=_random_tree(T, 2, T))
+    g = np.random.default_rng(T)
+    q = g.standard_normal(c.q.shape)
+    q[..., :32] = np.round(q[..., :32] * 300) * 2.0 ** -24
+    q[..., 32:] = np.clip(q[..., 32:] * 30000, -65504, 65504)
+    c.q = torch.from_numpy(q).to(torch.float16)
+    for n, by in ((slice(0, 1), 15), (slice(1, None), -15)):
+        s = c.host["k_scales"][..., n]
+        c.host["k_scales"][..., n] = np.where(s == 255, 255, s.astype(int) + by)
+    c.args["k_scales"] = torch.from_numpy(c.host["k_scales"]).cuda()
+    c.check(*c.run())
+    assert len(c.q[c.q.abs() < 2.0 ** -14].unique()) > 100  # (subnormal ones)
