@@ -345,8 +345,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const void* k_scales
  *
  * fa_cache_fork: the batch of the next step.  New sequence i continues old sequence parents[i] (outside 0 .. B - 1: it is empty):
  * new_lens[i] is the old length, and row i of new_table has the old row's pages up to it and -1 behind.  Whole pages are shared.  Of a
- * last page that is not full, the first new sequence keeps the page, if none has it as a whole one; the others get a free one each,
- * and (src, dst)[i] says so.  So sequences branch, change places and end by their parents alone, and what no new sequence has is
+ * last page that is not full, the first new sequence keeps the page, if it is not held and none has it as a whole one; the others get a
+ * free one each, and (src, dst)[i] says so.  So sequences branch, change places and end by their parents alone, and what no new sequence has is
  * free.  (Pages that the old table has behind a sequence's length are not taken over.)  Contents are to be copied before anything is
  * written to the new sequences.
  *   parents   : int32 [B_new];  new_table: int32 [B_new, max_pages];  new_lens, src, dst: int32 [B_new].  (new_table = block_table

@@ -20,7 +20,7 @@ def fork(table, lens, parents, held, page_size, n_pages):
     for row, n in zip(rows, new_lens):
         pair = (-1, -1)
         if n % page_size and 0 <= row[-1] < n_pages:
-            if row[-1] in whole or row[-1] in kept:
+            if row[-1] in whole or row[-1] in kept or (held is not None and held[row[-1]] != 0):
                 if free:
                     pair = (row[-1], free.pop(0))
                 else:

@@ -564,7 +564,8 @@ def _check_table(block_table):
 def fa_cache_fork(block_table, lens, parents, page_size, n_pages, held=None, new_table=None, new_lens=None, src=None, dst=None, missing=None,
                   workspace=None):
     """The batch of the next step: new_table [B_new,max_pages] and new_lens of sequences that continue parents[i] (int32 [B_new]; none: -1),
-    sharing whole pages; what fa_cache_copy has to copy for them (src, dst); and how many pages were missing."""
+    sharing whole pages; what fa_cache_copy has to copy for them (src, dst: last pages that are not full and have another reader, or are held);
+    and how many pages were missing."""
     if _native is not None:
         r = _native.cache_fork(block_table, lens, parents, page_size, n_pages, held, new_table, new_lens, src, dst, missing, workspace, _stream)
         if r is not None:

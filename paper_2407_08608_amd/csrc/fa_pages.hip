@@ -192,7 +192,9 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
     int *const part = lists.part, *const need = lists.need, *const list = lists.free;
     const int tid = threadIdx.x;
 
-    // The pages that new sequences would write to, and whether an earlier one does: that keeps it, the others need a copy
+    // The pages that new sequences would write to, and whether an earlier one does: that keeps it, the others need a copy.  Of a held page
+    // all do: who holds it reads it, and may go on from it.
+    auto held = [&](int page) __attribute__((always_inline)) { return pool.held && pool.held[page] != 0; };
     const bool once = a.B <= kListed;  // what is whole of each old sequence that is continued is written down here, and not for each window again
     if (once) {
         if (tid < a.B) s.whole[tid] = 0;
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
             const int page = part[tid];
             bool earlier = false;
             for (int j = 0; j < tid; ++j) earlier |= s.seen[j] == page;
-            need[tid] = page >= 0 && earlier;
+            need[tid] = page >= 0 && (earlier || held(page));
         }
     } else {
         int* const first = lists.high;
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
         __threadfence();
         __syncthreads();
         for (int i = tid; i < a.B_new; i += kThreads)
-            need[i] = part[i] >= 0 && __hip_atomic_load(&first[part[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i;
+            need[i] = part[i] >= 0 && (__hip_atomic_load(&first[part[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i || held(part[i]));
     }
 
     int found = 0;
