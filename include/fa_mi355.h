@@ -310,8 +310,9 @@ int fa_rope_frequencies(double* inv_freq, float* amplitude, int rot_dim, double 
  *     scale = a / 448,   code = round-to-nearest-even e4m3 of clamp(x * (448 / a), +-448),   a = max |x| over its finite elements
  * (a = 0: scale 1; 0 < a < 2^-100: a = 2^-100).  So an infinity becomes the largest value of the token, and a NaN stays one.
  * In an e2m1 cache each 32 elements of a row get
- *     scale = the least power of two s >= 2^-100 with a <= 7 s,   code = round-to-nearest-even e2m1 of clamp(x / s, +-6),   a as above
- * of those 32.  So no element is off by more than half a step, an infinity becomes +-6 s, and a NaN makes the byte of its scale 255.
+ *     scale = the least power of two s >= 2^-100 with a <= 7 s, or 2^125,   code = round-to-nearest-even e2m1 of clamp(x / s, +-6),   a as
+ * above of those 32.  So no element is off by more than half a step, but for those past 7 2^125, which become 6 2^125 (the largest that fp32
+ * has of the form); an infinity becomes +-6 s, and a NaN makes the byte of its scale 255.
  */
 #define FA_CACHE_MAX_PLACES 0x7fff0000
 

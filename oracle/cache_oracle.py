@@ -84,7 +84,7 @@ def quantise_groups(x):
     g = np.asarray(x, dtype=np.float64).reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
     a = np.where(np.isfinite(g), np.abs(g), 0.0).max(axis=-1)
     e = np.full(a.shape, -100)
-    for n in range(-100, 128):  # the least power of two with a <= 7 of it
+    for n in range(-100, 125):  # the least power of two with a <= 7 of it, but 2^125 at most
         e = np.where(a > 7 * 2.0 ** n, n + 1, e)
     codes = e2m1_encode(g / (2.0 ** e.astype(np.float64))[..., None]).reshape(x.shape)
     return codes[..., 0::2] | codes[..., 1::2] << 4, np.where(np.isnan(g).any(axis=-1), 255, e + 127).astype(np.uint8)

@@ -185,7 +185,7 @@ static __device__ __forceinline__ uint32_t largest_of_32(const Elements<DTYPE>& 
 }
 
 // 16 elements as codes, and the biased exponent of the scale that they share with the neighbouring lane's 16: of the least power of two s
-// with a <= 7 s, where 7 is what still rounds to the largest code, 6, by no more than half a step.  The conversions do the division,
+// with a <= 7 s, where 7 is what still rounds to the largest code, 6, by no more than half a step.  It is 2^125 at most: 4 2^126 is past fp32.  The conversions do the division,
 // round to nearest even and take what is more than 5, infinities too, to 6.
 template <int DTYPE>
 static __device__ __forceinline__ uint32_t quantise_32(const Elements<DTYPE>& x, Elements<FA_FP4_E2M1>& y) {
@@ -194,7 +194,7 @@ static __device__ __forceinline__ uint32_t quantise_32(const Elements<DTYPE>& x,
     const bool nan = top > inf;
     if (__builtin_expect(top >= inf, 0)) top = largest_of_32<true>(x);
     const uint32_t bits = DTYPE == FA_F32 ? top : DTYPE == FA_BF16 ? top << 16 : __builtin_bit_cast(uint32_t, Elem<f16_tag>::to_float((uint16_t)top));
-    const uint32_t biased = max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x600000u), 27);  // (no less than 2^-100)
+    const uint32_t biased = min(max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x600000u), 27), 252);  // (no less than 2^-100)
     y.set(x, power_of_two(biased));
     return nan ? 255 : biased;
 }
