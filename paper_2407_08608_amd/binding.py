@@ -426,12 +426,14 @@ def fa_rope_axes_bwd(dq, inv_freq, axis, positions, k=None, rot_dim=None, interl
 _CACHE_CODE = {torch.bfloat16: FA_BF16, torch.float16: FA_F16, torch.uint8: FA_FP8_E4M3, torch.float8_e4m3fn: FA_FP8_E4M3}
 
 
-_POWERS = (torch.uint8, torch.float8_e8m0fnu)
+# (Not every torch has these types; bytes it always takes.)
+_POWERS = tuple(t for t in (torch.uint8, getattr(torch, "float8_e8m0fnu", None)) if t is not None)
+_CODES4 = getattr(torch, "float4_e2m1fn_x2", None)
 
 
 def _in_four_bits(k_pages, k_scales):
     """Whether the last dimension of pages is half of d: two e2m1 codes to a byte, which their type says, or that of the scales does"""
-    return k_pages.dtype is torch.float4_e2m1fn_x2 or (k_pages.dtype is torch.uint8 and k_scales is not None and k_scales.dtype in _POWERS)
+    return (_CODES4 is not None and k_pages.dtype is _CODES4) or (k_pages.dtype is torch.uint8 and k_scales is not None and k_scales.dtype in _POWERS)
 
 
 def _check_pages(H_kv, d, k_pages, v_pages, k_scales, v_scales):
