@@ -574,9 +574,14 @@ int launch_cache_copy(const Cache& cache, const int* src, const int* dst, int n,
     const long scale_bytes = rows * (cache.dtype == FA_FP4_E2M1 ? d / 32 : cache.dtype == FA_FP8_E4M3 ? 4 : 0);
     auto go = [&](auto at_once, auto kernel) {
         const long each = 4096 * decltype(at_once)::value, chunks = (bytes + each - 1) / each;
-        if ((double)n * 2 * chunks * 256 >= 4294967296.0) return (int)FA_ERR_LAUNCH;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(n * 2 * chunks)), dim3(256), 0, stream, cache, src, dst, (unsigned)chunks, bytes, scale_bytes);
-        return launched();
+        const long most = 0xffffffffL / (256 * 2 * chunks);  // pairs of a launch: a grid has fewer than 2^32 threads
+        if (most == 0) return (int)FA_ERR_LAUNCH;
+        for (long first = 0; first < n; first += most) {
+            const long pairs = n - first < most ? n - first : most;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * 2 * chunks)), dim3(256), 0, stream, cache, src + first, dst + first, (unsigned)chunks, bytes, scale_bytes);
+            if (launched() != FA_OK) return (int)FA_ERR_LAUNCH;
+        }
+        return (int)FA_OK;
     };
     if ((double)n * 2 * bytes > 64.0 * 1024 * 1024) return go(std::integral_constant<int, 4>{}, fa_cache_copy_kernel<4>);
     return go(std::integral_constant<int, 2>{}, fa_cache_copy_kernel<2>);

@@ -48,3 +48,21 @@ def test_two_batches_that_go_on_from_one_prompt():
             assert torch.equal(x[:, :, :prompt], old.expand(table.shape[0], -1, -1, -1)) and torch.equal(x[:, :, prompt:], more)
     for x, old in zip(binding.fa_cache_read(k, v, store, _ints([prompt]), N=prompt), said):
         assert torch.equal(x, old)
+
+
+@pytest.mark.parametrize("n", [2 ** 23 - 1, 2 ** 23, 2 ** 23 + 5, 3 * 2 ** 23])
+def test_more_pairs_than_a_launch_takes(n):
+    # small pages, a pair to two workgroups: a grid ends at 2^23 - 1 pairs
+    n_pages = 40
+    g = torch.Generator(device="cuda").manual_seed(n % 1000)
+    have = [torch.randint(0, 256, (n_pages, 1, 16, x), generator=g, device="cuda", dtype=torch.uint8) for x in (32, 32, 2, 2)]
+    want = [t.clone() for t in have]
+    src, dst = torch.full((n,), -1, dtype=torch.int32, device="cuda"), torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    for i, at in enumerate((0, 1, 2 ** 23 - 2, min(2 ** 23 - 1, n - 2), n // 2, n - 1)):
+        src[at], dst[at] = i, 20 + i
+    for a, b in zip(src[src >= 0].tolist(), dst[src >= 0].tolist()):  # (the second at a place is the one that is there)
+        for t in want:
+            t[b] = t[a]
+    binding.fa_cache_copy(have[0], have[1], src, dst, k_scales=have[2], v_scales=have[3])
+    for a, b in zip(have, want):
+        assert torch.equal(a, b)
