@@ -17,7 +17,7 @@ namespace fa {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;  // (numbers that go up by this, or by a window, may pass 2^31 at the end: they have no sign)
 constexpr int kWindow = 1 << 18;  // pages whose bits are in the LDS at a time
 constexpr int kListed = 1024;     // rows whose numbers are kept in the LDS and not in the workspace
 constexpr int kSmallPool = 4096;  // pages whose lists are
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
         if (tid < a.B) s.whole[tid] = 0;
         __syncthreads();
     }
-    for (int i = tid; i < a.B_new; i += kThreads) {
+    for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads) {
         const Continued c(a, i);
         if (once && c.parent >= 0) s.whole[c.parent] = c.whole;  // (the same from all)
         const int page = c.last ? a.table[(long)c.parent * pool.max_pages + c.whole] : -1;
@@ -217,30 +217,30 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
         }
     } else {
         int* const first = lists.high;
-        for (int i = tid; i < a.B_new; i += kThreads)
+        for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads)
             if (part[i] >= 0) first[part[i]] = 0x7fffffff;
         __threadfence();
         __syncthreads();
-        for (int i = tid; i < a.B_new; i += kThreads)
-            if (part[i] >= 0) atomicMin(&first[part[i]], i);
+        for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads)
+            if (part[i] >= 0) atomicMin(&first[part[i]], (int)i);
         __threadfence();
         __syncthreads();
-        for (int i = tid; i < a.B_new; i += kThreads)
-            need[i] = part[i] >= 0 && (__hip_atomic_load(&first[part[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i || held(part[i]));
+        for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads)
+            need[i] = part[i] >= 0 && (__hip_atomic_load(&first[part[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int)i || held(part[i]));
     }
 
     int found = 0;
-    for (int base = 0; base < pool.n_pages; base += kWindow) {
-        const int n = min(kWindow, pool.n_pages - base);
+    for (unsigned window = 0; window < (unsigned)pool.n_pages; window += kWindow) {
+        const int base = (int)window, n = min(kWindow, pool.n_pages - base);
         clear(s.bits, (n + 31) / 32);
         // The whole pages of old sequences that are continued, each looked at once however many continue it: a wave takes 512 entries of a
         // row, two rows' at a time
-        for (int r0 = 0; r0 < a.B; r0 += kListed) {
-            const int rows = min(kListed, a.B - r0);
+        for (unsigned first_row = 0; first_row < (unsigned)a.B; first_row += kListed) {
+            const int r0 = (int)first_row, rows = min(kListed, a.B - r0);
             if (!once) {
                 for (int i = tid; i < rows; i += kThreads) s.whole[i] = 0;
                 __syncthreads();
-                for (int i = tid; i < a.B_new; i += kThreads) {
+                for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads) {
                     const Continued c(a, i);
                     if (c.parent >= r0 && c.parent - r0 < rows) s.whole[c.parent - r0] = c.whole;
                 }
@@ -265,10 +265,10 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
             }
             __syncthreads();
         }
-        for (int i = tid; i < a.B_new; i += kThreads)
+        for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads)
             if (part[i] >= base && part[i] - base < n && marked(s.bits, part[i], base)) need[i] = 1;  // a whole page of another: not to be written to
         __syncthreads();
-        for (int i = tid; i < a.B_new; i += kThreads) mark(s.bits, part[i], base, n);
+        for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads) mark(s.bits, part[i], base, n);
         mark_held(s.bits, pool, base, n);
         __syncthreads();
         collect(s.bits, nullptr, false, base, n, list, a.B_new, found, s.sums);
@@ -276,13 +276,13 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
     }
 
     int before = 0;
-    for (int r0 = 0; r0 < a.B_new; r0 += kThreads) {
-        const int i = r0 + tid;
-        const int needs = i < a.B_new ? need[i] : 0;
+    for (unsigned r0 = 0; r0 < (unsigned)a.B_new; r0 += kThreads) {
+        const unsigned i = r0 + tid;
+        const int needs = i < (unsigned)a.B_new ? need[i] : 0;
         int all;
         const int at = before + sum_before(needs, all, s.sums);
         before += all;
-        if (i >= a.B_new) continue;
+        if (i >= (unsigned)a.B_new) continue;
         const Continued c(a, i);
         const int page = needs && at < found ? list[at] : -1;
         a.new_lens[i] = c.len;
@@ -335,37 +335,37 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
     static_assert(kMany > kOwnEntries * kThreads);
     int* mine = nullptr;
     int n_mine = 0;
-    auto by_sequences = [&](int b0, int& all) __attribute__((always_inline)) {
-        const int b = b0 + tid;
+    auto by_sequences = [&](unsigned b0, int& all) __attribute__((always_inline)) {
+        const unsigned b = b0 + tid;
         int first = 0, last = -1, past = 0;
-        if (b < a.B) past = entries(b, first, last);
+        if (b < (unsigned)a.B) past = entries(b, first, last);
         mine = a.table + (long)b * pool.max_pages + first;
         n_mine = max(last - first + 1, 0);
         return sum_before(n_mine <= kOwnEntries && past == 0 ? none(mine, n_mine) : kMany, all, s.sums);
     };
     int all_past = 0;
     auto by_entries = [&](auto&& f) __attribute__((always_inline)) {
-        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-            const int b = b0 + tid;
+        for (unsigned b0 = 0; b0 < (unsigned)a.B; b0 += kThreads) {
+            const unsigned b = b0 + tid;
             int first = 0, last = -1, all;
-            if (b < a.B) all_past += entries(b, first, last);
+            if (b < (unsigned)a.B) all_past += entries(b, first, last);
             const int before = sum_before(max(last - first + 1, 0), all, s.sums);
             s.seen[tid] = before;
             s.whole[tid] = first;
             __syncthreads();
-            for (int i0 = 0; i0 < all; i0 += kThreads) {
-                const int i = i0 + tid;
+            for (unsigned i0 = 0; i0 < (unsigned)all; i0 += kThreads) {
+                const unsigned i = i0 + tid;
                 int row = 0;  // the last that begins with entry i or before
 #pragma unroll
-                for (int step = kThreads / 2; step > 0; step /= 2) row += s.seen[row + step] <= i ? step : 0;
-                f(a.table + (long)(b0 + row) * pool.max_pages + s.whole[row] + i - s.seen[row], i < all ? 1 : 0);
+                for (int step = kThreads / 2; step > 0; step /= 2) row += (unsigned)s.seen[row + step] <= i ? step : 0;
+                f(a.table + (long)(b0 + row) * pool.max_pages + s.whole[row] + i - s.seen[row], i < (unsigned)all ? 1 : 0);
             }
             __syncthreads();
         }
     };
     int wanted = 0, beyond = 0, at = 0;
     bool any_many = false;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    for (unsigned b0 = 0; b0 < (unsigned)a.B; b0 += kThreads) {
         int all;
         at = by_sequences(b0, all);
         wanted += all % kMany;
@@ -384,8 +384,8 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
     const int asked = min(wanted, pool.n_pages);
     int* const list = lists_of(s, a.workspace, a.B, pool.n_pages, 1).free;
     int found = 0;
-    for (int base = 0; base < pool.n_pages; base += kWindow) {
-        const int n = min(kWindow, pool.n_pages - base);
+    for (unsigned window = 0; window < (unsigned)pool.n_pages; window += kWindow) {
+        const int base = (int)window, n = min(kWindow, pool.n_pages - base);
         clear(s.bits, (n + 31) / 32);
         mark_table(s.bits, a.table, a.B * pool.max_pages, base, n);
         mark_held(s.bits, pool, base, n);
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_extend_kernel(ExtendArgs a)
             give(entry, n, from, list, most);
         });
     } else {
-        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        for (unsigned b0 = 0; b0 < (unsigned)a.B; b0 += kThreads) {
             if (a.B > kThreads) {
                 int all;
                 at = before + by_sequences(b0, all);
@@ -435,8 +435,8 @@ __global__ void __launch_bounds__(kThreads) fa_cache_compact_kernel(CompactArgs 
     const int tid = threadIdx.x, half = bitmap_words(pool.n_pages);
     uint32_t *const used = s.bits, *const held = s.bits + half;
     int n_free = 0, n_high = 0, top_held = -1;
-    for (int base = 0; base < pool.n_pages; base += kWindow) {
-        const int n = min(kWindow, pool.n_pages - base);
+    for (unsigned window = 0; window < (unsigned)pool.n_pages; window += kWindow) {
+        const int base = (int)window, n = min(kWindow, pool.n_pages - base);
         clear(used, half);
         clear(held, half);
         mark_table(used, a.table, a.B * pool.max_pages, base, n);
@@ -454,19 +454,19 @@ __global__ void __launch_bounds__(kThreads) fa_cache_compact_kernel(CompactArgs 
     const int most = min(min(n_free, n_high), a.moves);
     int mine = 0, moved;
     constexpr int AHEAD = 4;
-    for (int k0 = tid; k0 < a.moves; k0 += AHEAD * kThreads) {
+    for (unsigned k0 = tid; k0 < (unsigned)a.moves; k0 += AHEAD * kThreads) {
         int from[AHEAD], to[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int k = k0 + j * kThreads;
-            from[j] = k < most ? lists.high[n_high - 1 - k] : -1;
-            to[j] = k < most ? lists.free[k] : 0;
+            const unsigned k = k0 + j * kThreads;
+            from[j] = k < (unsigned)most ? lists.high[n_high - 1 - k] : -1;
+            to[j] = k < (unsigned)most ? lists.free[k] : 0;
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int k = k0 + j * kThreads;
+            const unsigned k = k0 + j * kThreads;
             const bool moves = to[j] < from[j];  // (once one does not, none after it does)
-            if (k < a.moves) {
+            if (k < (unsigned)a.moves) {
                 a.src[k] = moves ? from[j] : -1;
                 a.dst[k] = moves ? to[j] : -1;
             }
