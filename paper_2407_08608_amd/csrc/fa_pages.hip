@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
     // The pages that new sequences would write to, and whether an earlier one does: that keeps it, the others need a copy.  Of a held page
     // all do: who holds it reads it, and may go on from it.
     auto held = [&](int page) __attribute__((always_inline)) { return pool.held && pool.held[page] != 0; };
-    const bool once = a.B <= kListed;  // what is whole of each old sequence that is continued is written down here, and not for each window again
+    const bool once = a.B <= kListed;  // what is whole of each old sequence that is continued is written down here
     if (once) {
         if (tid < a.B) s.whole[tid] = 0;
         __syncthreads();
@@ -234,27 +234,19 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
         const int base = (int)window, n = min(kWindow, pool.n_pages - base);
         clear(s.bits, (n + 31) / 32);
         // The whole pages of old sequences that are continued, each looked at once however many continue it: a wave takes 512 entries of a
-        // row, two rows' at a time
-        for (unsigned first_row = 0; first_row < (unsigned)a.B; first_row += kListed) {
-            const int r0 = (int)first_row, rows = min(kListed, a.B - r0);
-            if (!once) {
-                for (int i = tid; i < rows; i += kThreads) s.whole[i] = 0;
-                __syncthreads();
-                for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads) {
-                    const Continued c(a, i);
-                    if (c.parent >= r0 && c.parent - r0 < rows) s.whole[c.parent - r0] = c.whole;
-                }
-                __syncthreads();
-            }
+        // row, two rows' at a time.  Of more old sequences than are written down, the entries of the new ones, so the work goes by their
+        // number: us, 1024 old ones at a time with all new ones looked at for each / so, 1025 rows of 40 entries 67 / 32, 8192 of 33 continued by
+        // 1500 728 / 59, 2048 of 257 by parents at random 304 / 340; a million and more of one entry: minutes / below a second.
+        if (once) {
             const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), parts = (pool.max_pages + 511) / 512;
-            const unsigned units = (unsigned)rows * parts;
+            const unsigned units = (unsigned)a.B * parts;
             for (unsigned u0 = wave; u0 < units; u0 += 2 * kWaves) {
                 int page[2][8];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const unsigned u = min(u0 + x * kWaves, units - 1);
                     const int row = u / (unsigned)parts, e0 = (u - row * parts) * 512 + lane, whole = s.whole[row];
-                    const int* const entries = a.table + (long)(r0 + row) * pool.max_pages;
+                    const int* const entries = a.table + (long)row * pool.max_pages;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) page[x][j] = e0 + 64 * j < whole ? entries[e0 + 64 * j] : -1;
                 }
@@ -263,8 +255,39 @@ __global__ void __launch_bounds__(kThreads) fa_cache_fork_kernel(ForkArgs a) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) mark(s.bits, page[x][j], base, n);
             }
-            __syncthreads();
+        } else {
+            constexpr int AHEAD = 8;
+            static_assert(kListed == kThreads);
+            const int more_rows = kThreads / (unsigned)pool.max_pages, more = kThreads - more_rows * pool.max_pages;  // from a thread's entry to its next
+            for (unsigned r0 = 0; r0 < (unsigned)a.B_new; r0 += kListed) {
+                const unsigned rows = min((unsigned)kListed, a.B_new - r0), entries = rows * pool.max_pages;
+                if (tid < (int)rows) {
+                    const Continued c(a, (int)(r0 + tid));
+                    s.seen[tid] = c.parent;
+                    s.whole[tid] = c.whole;
+                }
+                __syncthreads();
+                unsigned row = tid / (unsigned)pool.max_pages;
+                int e = tid - row * pool.max_pages;
+                for (unsigned i0 = tid; i0 < entries; i0 += AHEAD * kThreads) {
+                    int page[AHEAD];
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) {
+                        page[j] = i0 + j * kThreads < entries && e < s.whole[row] ? a.table[(long)s.seen[row] * pool.max_pages + e] : -1;
+                        row += more_rows;
+                        e += more;
+                        if (e >= pool.max_pages) {
+                            e -= pool.max_pages;
+                            ++row;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) mark(s.bits, page[j], base, n);
+                }
+                __syncthreads();
+            }
         }
+        __syncthreads();
         for (unsigned i = tid; i < (unsigned)a.B_new; i += kThreads)
             if (part[i] >= base && part[i] - base < n && marked(s.bits, part[i], base)) need[i] = 1;  // a whole page of another: not to be written to
         __syncthreads();

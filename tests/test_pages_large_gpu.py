@@ -1,4 +1,5 @@
-"""Pages of a pool at the largest numbers that the calls take: as many pages and moves as an int counts."""
+"""Pages of a pool at the largest numbers that the calls take: many sequences, as many pages and moves as an int counts."""
+import numpy as np
 import pytest
 import torch
 
@@ -14,6 +15,23 @@ MOST = 2 ** 31 - 1
 def _memory_goes_back():
     yield
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("last", [16, 5])
+def test_fork_of_millions(last):
+    """The work goes by the new sequences' entries, not by their number times the old ones'"""
+    B, n_pages = 1 << 21, 3 << 20
+    g = np.random.default_rng(last)
+    page = g.permutation(n_pages)[:B]
+    parents = g.permutation(B)
+    parents[B // 2:B // 2 + 1000] = parents[:1000]  # these need a copy where the page is not full
+    got = binding.fa_cache_fork(_ints(page[:, None]), _ints(np.full(B, last)), _ints(parents), 16, n_pages)
+    rows, src, dst = page[parents], np.full(B, -1), np.full(B, -1)
+    if last < 16:
+        free = np.setdiff1d(np.arange(n_pages), rows)[:1000]
+        src[B // 2:B // 2 + 1000], dst[B // 2:B // 2 + 1000] = rows[:1000], free
+        rows = np.where(dst >= 0, dst, rows)
+    _same(got, (rows, np.full(B, last), src, dst, 0))
 
 
 def test_as_many_moves_as_an_int_counts():
