@@ -66,3 +66,47 @@ def test_more_pairs_than_a_launch_takes(n):
     binding.fa_cache_copy(have[0], have[1], src, dst, k_scales=have[2], v_scales=have[3])
     for a, b in zip(have, want):
         assert torch.equal(a, b)
+
+
+# rows, entries of a row, pages: beyond 16384 entries the table is renumbered by a launch of its own where the lists are in a workspace
+@pytest.mark.parametrize("B,wide,n_pages", [(1, 16385, 5000), (3, 5463, 4097), (127, 129, 9001), (1025, 17, 4000), (7, 2341, 262145), (40, 411, 600001), (64, 257, 3000), (64, 256, 9001)])
+@pytest.mark.parametrize("held", [False, True])
+def test_large_tables_are_renumbered(B, wide, n_pages, held):
+    g = np.random.default_rng(B + wide)
+    table = g.integers(0, n_pages, (B, wide))
+    table[g.random((B, wide)) < 0.7] = -1
+    table = np.where(g.random((B, wide)) < 0.05, g.choice([-7, n_pages, 2 ** 31 - 1, -2 ** 31], (B, wide)), table)
+    table[0, 0], table[-1, -1] = n_pages - 1, n_pages - 2
+    keep = (g.random(n_pages) < 0.2) * g.choice([1, -4]) if held else None
+    h = None if keep is None else _ints(keep)
+    space = torch.empty(max(binding.fa_cache_pages_workspace_bytes(B, n_pages), 16), dtype=torch.uint8, device="cuda").random_(0, 256)
+    for moves in (n_pages // 2, 1, 700, 0):
+        want = pages_oracle.compact(table, keep, n_pages, moves or n_pages)
+        if moves:
+            _same(binding.fa_cache_compact(_ints(table), n_pages, moves=moves, held=h, workspace=space), want)
+        else:  # in place, from a table whose entries are not aligned to 16 bytes
+            t = torch.zeros(B * wide + 1, dtype=torch.int32, device="cuda")[1:].view(B, wide).copy_(_ints(table))
+            got = binding.fa_cache_compact(t, n_pages, moves=n_pages, held=h, new_table=t, workspace=space)
+            assert got[0] is t
+            _same(got, want)
+
+
+@pytest.mark.parametrize("B,B_new,wide,n_pages", [(3, 5, 513, 4000), (5, 9, 1025, 4096), (4, 40, 1025, 9000), (1024, 1100, 513, 600000), (1025, 700, 513, 600000), (2050, 1500, 3, 7000),
+                                                  (1100, 1200, 1025, 300000)])
+@pytest.mark.parametrize("held", [False, True])
+def test_forks_of_wide_rows(B, B_new, wide, n_pages, held):
+    """Lengths on both sides of entries 512 and 1024, free pages that only marks from there on decide about"""
+    g = np.random.default_rng(B + wide)
+    page = 16
+    pool = g.permutation(n_pages)
+    table = pool[g.integers(0, min(n_pages, 3 * wide), (B, wide))]
+    table[:, :4] = -1
+    table[0, 512:] = np.sort(pool)[:max(wide - 512, 0)]  # the lowest pages: taken by what lies behind entry 511 alone
+    edges = [e * page + k for e in (511, 512, 513, 1023, 1024, 1025, wide - 1, wide) for k in (-1, 0, 1)]
+    lens = g.choice([n for n in edges + [0, 5, wide * page // 2] if 0 <= n <= wide * page], B)
+    lens[0] = wide * page
+    parents = g.integers(0, B, B_new)
+    parents[:3] = [0, B - 1, -1]
+    keep = (g.random(n_pages) < 0.2) * g.choice([1, -4]) if held else None
+    got = binding.fa_cache_fork(_ints(table), _ints(lens), _ints(parents), page, n_pages, held=None if keep is None else _ints(keep))
+    _same(got, pages_oracle.fork(table, lens, parents, keep, page, n_pages))
