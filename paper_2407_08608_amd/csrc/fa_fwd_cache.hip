@@ -1266,6 +1266,17 @@ static bool whole_sequences(double workgroups, int max_len) {
         const double limit = 8 * workgroups + 256 > 512 ? 8 * workgroups + 256 : 512;
         return max_len <= kAlone * 3 / 4 && max_len * (Form::D == 64 ? 1.1 : 1.25) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
     }
+    // The other forms of e2m1 go by the constants of 16-bit and e4m3 caches.  us, whole / teams, by workgroups and the longest of lengths spread
+    // over the last half (d = 256 of 4 rows: third), * where the rule takes the longer:
+    //   32 rows   d = 64   8: 512 8.3 / 10.3, 1024 11.3 / 10.4;  32: 1024 *11.2 / 13.1;  128: 2048 *19.9 / 16.2;  256: 4096 *36 / 30;  512: 2048 24 / 30
+    //             d = 128  8: 512 12.9 / 12.6, 1024 18 / 13;  128: 1024 18.5 / 19.5, 2048 29 / 23;  256: 2048 30 / 33, 4096 *52 / 44;  512: 2048 37 / 45
+    //             d = 256  8: 256 16 / 18, 512 19 / 18;  128: 1024 28 / 28;  256: 4096 74 / 88;  512: 2048 86 / 97
+    //   52 rows   d = 64   128: 1024 18 / 19, 2048 *29 / 26;  256: 4096 51 / 56;   d = 128  128: 2048 40 / 38;  256: 4096 71 / 80;  512: 2048 80 / 89
+    //   128 rows  d = 64   32: 512 17.1 / 17.6;  128: 1024 *29 / 28;  256: 1024 29 / 33, 2048 *53 / 45;  512: 2048 71 / 72
+    //             d = 128  128: 512 25 / 29, 1024 41 / 34;  256: 1024 42 / 51, 2048 73 / 67;  512: 2048 101 / 111
+    //             d = 256  128: 512 41 / 41;  256: 1024 69 / 98, 2048 *118 / 134, 4096 217 / 207;  512: 2048 229 / 229
+    //   4 rows    d = 256  128: 512 16.0 / 17.5, 1024 22 / 20;  256: 1024 23 / 27, 2048 37 / 39;  512: 2048 56 / 65
+    // (where 256 workgroups or 2048 keys are a little too many for whole sequences it loses up to a fifth, and is right elsewhere)
     constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
                      d256 = Form::COLS == 16 ? (Form::CODES ? 1.5 : 2.0) : shared ? 2.0 : 1.25;
     if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return max_len <= kAlone;
