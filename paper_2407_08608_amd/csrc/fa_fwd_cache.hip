@@ -1267,7 +1267,7 @@ static bool whole_sequences(double workgroups, int max_len) {
         return max_len <= kAlone * 3 / 4 && max_len * (Form::D == 64 ? 1.1 : 1.25) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
     }
     // The other forms of e2m1 go by the constants of 16-bit and e4m3 caches.  us, whole / teams, by workgroups and the longest of lengths spread
-    // over the last half (d = 256 of 4 rows: third), * where the rule takes the longer:
+    // over the last half (d = 256 of 4 rows: third); * before a pair: the rule takes the longer:
     //   32 rows   d = 64   8: 512 8.3 / 10.3, 1024 11.3 / 10.4;  32: 1024 *11.2 / 13.1;  128: 2048 *19.9 / 16.2;  256: 4096 *36 / 30;  512: 2048 24 / 30
     //             d = 128  8: 512 12.9 / 12.6, 1024 18 / 13;  128: 1024 18.5 / 19.5, 2048 29 / 23;  256: 2048 30 / 33, 4096 *52 / 44;  512: 2048 37 / 45
     //             d = 256  8: 256 16 / 18, 512 19 / 18;  128: 1024 28 / 28;  256: 4096 74 / 88;  512: 2048 86 / 97
@@ -1278,7 +1278,7 @@ static bool whole_sequences(double workgroups, int max_len) {
     //   4 rows    d = 256  128: 512 16.0 / 17.5, 1024 22 / 20;  256: 1024 23 / 27, 2048 37 / 39;  512: 2048 56 / 65
     // (where 256 workgroups or 2048 keys are a little too many for whole sequences it loses up to a fifth, and is right elsewhere)
     constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
-                     d256 = Form::COLS == 16 ? (Form::CODES ? 1.5 : 2.0) : shared ? 2.0 : 1.25;
+                     d256 = Form::COLS == 16 ? (Form::HELD == kWords ? 2.0 : 1.5) : shared ? 2.0 : 1.25;
     if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return max_len <= kAlone;
     const double limit = 8 * workgroups + 256 > 512 ? 8 * workgroups + 256 : 512;
     return max_len * (Form::D == 64 ? d64 : Form::D == 128 ? d128 : d256) <= limit * (Form::NW == 8 ? 1.8 : 1.0);
@@ -1293,7 +1293,6 @@ static bool whole_sequences(double workgroups, int max_len) {
 template <int D_, int HELD_, int COLS_, int RT_, int NW_, int FORM_>
 struct CachedForm {
     static constexpr int D = D_, HELD = HELD_, COLS = COLS_, RT = RT_, NW = NW_, FORM = FORM_, STG = FORM != kShareKeys ? 1 : HELD == kCodes4 ? 2 : 3;
-    static constexpr bool CODES = HELD != kWords;
     template <typename Tag>
     using Shape = CachedShape<Tag, D, HELD, COLS, RT, NW, STG, FORM>;
 };
