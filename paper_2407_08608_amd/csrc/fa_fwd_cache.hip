@@ -10,7 +10,7 @@
 // 32 sequences of 500 to 4096 keys, H = 32 on 8, bf16, T = 1: 268 MB in 51 us, 5.2 TB/s; 2 of up to 65536 keys, H = 16 on 2,
 // d = 256, codes: 129 MB in 33 us, of which some 13 are the look-up of pages, the merge and the join; 4 trees of 64 tokens over up to
 // 16384 keys, H = 32 on 4, bf16: 50 GFLOP in 91 us, where the matrix pipes are busy a third of the loop; over e2m1 the first in 24 us
-// (3.0 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 43.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
+// (3.0 TB/s), the second, of 50000 and more keys, in 31, 8 trees of 32 over 5000 to 8192 keys, H = 16 on 4, fp16: 9.7 GFLOP in 44.  A wave stages its own tiles (no barrier in the loop): a slot for K and one for V, STG deep,
 // refilled as soon as the wave has read them, so requests go on while scores, softmax and products are computed.
 //   - Work: the steps of all sequences and heads lie in a row, and each team of workgroups (one for each row group) takes an equal
 //     share of it, whatever the lengths are: they are known on the device only.  A share may end inside a sequence; what a team
@@ -1276,7 +1276,7 @@ static bool whole_sequences(double workgroups, int max_len) {
     //             d = 128  128: 512 25 / 29, 1024 41 / 34;  256: 1024 42 / 51, 2048 73 / 67;  512: 2048 101 / 111
     //             d = 256  128: 512 41 / 41;  256: 1024 69 / 98, 2048 *118 / 134, 4096 217 / 207;  512: 2048 229 / 229
     //   4 rows    d = 256  128: 512 16.0 / 17.5, 1024 22 / 20;  256: 1024 23 / 27, 2048 37 / 39;  512: 2048 56 / 65
-    // (where 256 workgroups or 2048 keys are a little too many for whole sequences it loses up to a fifth, and is right elsewhere)
+    // (of 216 such shapes the rule takes the longer by more than 5 % in 9, by 1.23 times at most)
     constexpr double d64 = Form::COLS == 16 ? 0.75 : shared ? 1.0 : 0.5, d128 = Form::COLS == 16 ? 1.0 : shared ? 1.5 : 0.75,
                      d256 = Form::COLS == 16 ? (Form::HELD == kWords ? 2.0 : 1.5) : shared ? 2.0 : 1.25;
     if (workgroups >= 512 || (workgroups >= 256 && Form::COLS == 32 && !shared)) return max_len <= kAlone;
