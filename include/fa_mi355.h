@@ -349,7 +349,8 @@ int fa_cache_read(const void* k_pages, const void* v_pages, const void* k_scales
  * last page that is not full, the first new sequence keeps the page, if it is not held and none has it as a whole one; the others get a
  * free one each, and (src, dst)[i] says so.  So sequences branch, change places and end by their parents alone, and what no new sequence has is
  * free.  (Pages that the old table has behind a sequence's length are not taken over.)  Contents are to be copied before anything is
- * written to the new sequences.
+ * written to the new sequences.  Where a page was missing, the new sequence's tokens of it are not there, and a page that fa_cache_extend
+ * gives it later does not hold them.
  *   parents   : int32 [B_new];  new_table: int32 [B_new, max_pages];  new_lens, src, dst: int32 [B_new].  (new_table = block_table
  *               or new_lens = lens: FA_ERR_SHAPE)
  *
