@@ -1,5 +1,8 @@
 """What attention over a 4-bit cache keeps of its operands, whatever the types and the number of rows: probabilities have 16 bits in their product
-with V, and a product of Q and K is exact, however far a row's scales are apart."""
+with V, and a product of Q and K is exact, however far a row's scales are apart.
+
+The bounds are those of Case: e_s = (2 d + 4) 2^-24 scale max_j sum |q k_j| holds for fp16 Q as two bf16 numbers h + r too.  That is exact, so are 2 d products,
+and their sum is off by 2 d 2^-24 sum (|h k| + |r k|) at most, where |h| + |r| <= (1 + 2^-7) |q|: 2 d 2^-7 <= 4 up to d = 256."""
 import numpy as np
 import pytest
 import torch
